@@ -264,6 +264,25 @@ int ddit_self_attn_fwd(ddit_attn_kind kind, const ddit_shape *shape, void *q, vo
                        int64_t ld_kv, const void *g_q, const void *g_k, float *rope_table_or_null, int fuse, void *o,
                        int64_t ld_o, float *lse_or_null, void *hip_stream);
 
+/* ---- operators of models that differ from the step's layers: norms behind a branch, linears in four bits, packed requests ---- */
+
+typedef enum { DDIT_NORM_LAYER = 0, DDIT_NORM_RMS = 1 } ddit_norm_kind;
+
+/* What stands between two branches of a model that normalises on both sides of each: the branch's output f is normalised, scaled,
+ * gated and added to the scaled stream, and the stream normalised and modulated for the next branch, in one pass:
+ *   x_out[n] = residual_scale * x[n] + gate_b * Norm(f[n]) * g_post
+ *   out[n]   = bf16( Norm(x_out[n]) * g_pre * (1 + scale_b) + shift_b )
+ * Norm over the D features: DDIT_NORM_LAYER (x - mean) / sqrt(var + eps) with the biased variance, DDIT_NORM_RMS
+ * x / sqrt(mean(x^2) + eps).  g_post, g_pre: bf16 [D], NULL = 1.  gate_b = row gate_row of gate_table + c6[b] (gate_row < 0: no
+ * gate); (shift_b, scale_b) = rows (3*which, 3*which+1) of next_table + c6[b] (which < 0: none); tables fp32 [6,D], c6 fp32
+ * [samples,6D], b = n / tokens_per_sample.  The two tables differ where the next branch belongs to the next layer.  f bf16 [N,D]
+ * with row stride ld_f, x and x_out fp32 [N,D], out bf16 [N,D] with row stride ld_out, or NULL for the stream alone.  x_out may be
+ * x; no other output may overlap an input.  N = 0 as above.  D up to 8192. */
+int ddit_branch_norms_fwd(int norm, const void *f, int64_t ld_f, const void *g_post_or_null, const float *x, float residual_scale,
+                          const float *gate_table, const float *c6, int gate_row, float *x_out, const void *g_pre_or_null,
+                          const float *next_table, int which, int64_t N, int64_t tokens_per_sample, int32_t D, float eps,
+                          void *out_or_null, int64_t ld_out, void *hip_stream);
+
 /* ---- output tiles of the linear: for tuning and for parity tests of every compiled tile ----
  * The linear is compiled for a short list of output tiles (rows x cols of out per workgroup), which callers can force, and for
  * a few forms beside the list.  ddit_linear_fwd takes, per call, a form for few tokens where its grid finds room on the device

@@ -20,6 +20,7 @@ DDIT_ERR_INVALID_ARG, DDIT_ERR_UNSUPPORTED, DDIT_ERR_WORKSPACE, DDIT_ERR_ALIGNME
 DDIT_ATTN_SPATIAL, DDIT_ATTN_TEMPORAL, DDIT_ATTN_CROSS = 0, 1, 2
 DDIT_EPI_BF16, DDIT_EPI_GELU_BF16, DDIT_EPI_RESIDUAL_F32 = 0, 1, 2
 DDIT_EPI_COPY = 16   # ddit_linear_tile_choice: a residual update that also writes bf16(x)
+DDIT_NORM_LAYER, DDIT_NORM_RMS = 0, 1
 DDIT_FLAG_TAPS, DDIT_FLAG_QK_NORM, DDIT_FLAG_ROPE_TEMPORAL = 1, 2, 4
 TAP_NAMES = ["xh_msa", "qkv", "o", "x_after_attn", "qc", "kvc", "oc", "x_after_cross", "xh_mlp", "h", "x_out"]
 _TAP_DTYPE = {"x_after_attn": torch.float32, "x_after_cross": torch.float32, "x_out": torch.float32}
@@ -32,7 +33,8 @@ EXPORTS = ["ddit_abi_version", "ddit_status_string", "ddit_last_error", "ddit_wo
            "ddit_linear_tile_info", "ddit_linear_tile_choice", "ddit_linear_form", "ddit_linear_few_form", "ddit_attn_form", "ddit_cross_kv_form", "ddit_linear_front_tokens", "ddit_linear_fwd_tile",
            "ddit_linear_partial_choice", "ddit_linear_partial_fwd", "ddit_qk_norm_rope_fwd", "ddit_self_attn_fwd", "ddit_optimal_dop",
            "ddit_buddy_create", "ddit_buddy_alloc", "ddit_buddy_release", "ddit_buddy_free_gpus", "ddit_buddy_destroy",
-           "ddit_sched_simulate", "ddit_probe_mfma_bf16", "ddit_probe_stream_copy", "ddit_probe_stream_read", "ddit_probe_residual_stream"]
+           "ddit_sched_simulate", "ddit_probe_mfma_bf16", "ddit_probe_stream_copy", "ddit_probe_stream_read", "ddit_probe_residual_stream",
+           "ddit_branch_norms_fwd"]
 
 
 class ddit_shape(C.Structure):
@@ -173,6 +175,8 @@ def _load() -> C.CDLL:
     lib.ddit_probe_stream_copy.argtypes = [VP, VP, C.c_int64, VP]
     lib.ddit_probe_stream_read.argtypes = [VP, C.c_int64, VP, VP]
     lib.ddit_probe_residual_stream.argtypes = [VP, VP, VP, VP, C.c_int64, C.c_int32, C.c_int32, VP]
+    lib.ddit_branch_norms_fwd.argtypes = [C.c_int, VP, C.c_int64, VP, VP, C.c_float, VP, VP, C.c_int, VP, VP, VP, C.c_int, C.c_int64,
+                                          C.c_int64, C.c_int32, C.c_float, VP, C.c_int64, VP]
     for n in EXPORTS:
         if n not in ("ddit_abi_version", "ddit_status_string", "ddit_last_error", "ddit_linear_tile_count"):
             getattr(lib, n).restype = C.c_int
@@ -522,6 +526,14 @@ def ddit_sample(shape: ddit_shape, weights: ddit_step_weights, io: ddit_io_weigh
     _check(_lib.ddit_sample(C.byref(shape), C.byref(weights), C.byref(io), _ptr(z), _ptr(y), _i32(y_valid_len),
                             _ptr(y_uncond), _ptr(cross_kv), _ptr(cross_kv_uncond), guidance, n_steps, first_step,
                             last_step, _ptr(eps_scratch), _ptr(workspace), _nbytes(workspace), _stream()))
+
+
+def ddit_branch_norms_fwd(norm: int, f, ld_f: int, g_post, x, residual_scale: float, gate_table, c6, gate_row: int, x_out, g_pre, next_table,
+                          which: int, tokens_per_sample: int, eps: float, out, ld_out: int) -> None:
+    N, D = x.shape[0], x.shape[1]
+    _check(_lib.ddit_branch_norms_fwd(norm, _ptr(f), ld_f, _ptr(g_post), _ptr(x), residual_scale, _ptr(gate_table), _ptr(c6), gate_row,
+                                      _ptr(x_out), _ptr(g_pre), _ptr(next_table), which, N, tokens_per_sample, D, eps, _ptr(out), ld_out,
+                                      _stream()))
 
 
 def ddit_probe_mfma_bf16(operands, sink, iters: int) -> float:

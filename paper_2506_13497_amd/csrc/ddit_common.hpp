@@ -3,6 +3,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "prefetch.hpp"
 
 typedef __bf16 bf16_t;
@@ -53,6 +55,8 @@ __device__ __forceinline__ void prefetch_share(const Prefetch &f) {
 namespace ddit {
 void set_error(const char *fmt, ...);
 int hip_fail(hipError_t e, const char *what);
+// Lets a kernel take more than 48 KB of dynamic LDS on the current device; asked once per device (a bit of *done each).
+int allow_dynamic_lds(const void *kernel, int bytes, std::atomic<uint64_t> *done);
 int device_cus();   // compute units of the current device (cached per process; 256 if there is no device)
 
 // kernel launchers (each validates nothing: callers have validated shapes)
@@ -175,6 +179,19 @@ struct CondArgs {
 int launch_timestep_conditioning(const CondArgs &c, const void *w_t1, const void *b_t1, const void *w_t2,
                                  const void *b_t2, const void *w_ada, const void *b_ada, const float *temb_in,
                                  float *c6_out, float *scratch, hipStream_t s);
+
+// norms on both sides of a residual branch (branch_norms.hip)
+struct BranchNormsArgs {
+  int norm;                            // 0 LayerNorm, 1 RMS norm
+  const void *f; int64_t ld_f;         // bf16 [N, D]
+  const void *g_post, *g_pre;          // bf16 [D] or null
+  const float *x; float residual_scale; float *x_out;   // fp32 [N, D]; may be the same
+  const float *gate_tab, *gate_c6;     // row of a table, the same row of sample 0's conditioning; null: no gate
+  const float *mod_tab, *mod_c6;       // the shift row of both, the scale row behind it; null: no modulation
+  int64_t N, tokens_per_sample; int D; float eps;
+  void *out; int64_t ld_out;           // bf16 [N, D] or null
+};
+int launch_branch_norms(const BranchNormsArgs &a, hipStream_t s);
 
 // layers around the token-space step, solver
 int launch_position_code(float *pos, int Hp, int Wp, int D, hipStream_t s);

@@ -27,6 +27,17 @@ int hip_fail(hipError_t e, const char *what) {
   return DDIT_ERR_HIP;
 }
 
+int allow_dynamic_lds(const void *kernel, int bytes, std::atomic<uint64_t> *done) {
+  int dev = 0;
+  int rc = hip_fail(hipGetDevice(&dev), "hipGetDevice");
+  if (rc != DDIT_OK) return rc;
+  const uint64_t bit = dev < 64 ? (uint64_t)1 << dev : 0;
+  if (bit && (done->load(std::memory_order_acquire) & bit)) return DDIT_OK;
+  rc = hip_fail(hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes), "hipFuncSetAttribute");
+  if (rc == DDIT_OK) done->fetch_or(bit, std::memory_order_release);
+  return rc;
+}
+
 int device_cus() {
   static int cus = 0;   // benign race: every thread computes the same value
   if (cus == 0) {
@@ -853,6 +864,39 @@ int ddit_self_attn_fwd(ddit_attn_kind kind, const ddit_shape *shape, void *q, vo
     tab = rope_table_or_null;
   }
   return run_self_attention(kind, d, q, k, v, ld_q, ld_kv, g_q, g_k, shape->ln_eps, tab, fuse != 0, o, ld_o, lse_or_null, s);
+}
+
+int ddit_branch_norms_fwd(int norm, const void *f, int64_t ld_f, const void *g_post_or_null, const float *x, float residual_scale,
+                          const float *gate_table, const float *c6, int gate_row, float *x_out, const void *g_pre_or_null,
+                          const float *next_table, int which, int64_t N, int64_t tokens_per_sample, int32_t D, float eps, void *out_or_null,
+                          int64_t ld_out, void *hip_stream) {
+  if (norm != DDIT_NORM_LAYER && norm != DDIT_NORM_RMS) { set_error("unknown norm %d", norm); return DDIT_ERR_INVALID_ARG; }
+  if (!f || !x || !x_out) { set_error("f, x and x_out must not be NULL"); return DDIT_ERR_INVALID_ARG; }
+  if (N < 0 || tokens_per_sample < 1 || D < 1 || !(eps > 0.f) || gate_row > 5 || which > 1) {
+    set_error("branch_norms: N=%lld tokens_per_sample=%lld D=%d eps=%g gate_row=%d which=%d", (long long)N, (long long)tokens_per_sample, D,
+              (double)eps, gate_row, which);
+    return DDIT_ERR_INVALID_ARG;
+  }
+  if (!(residual_scale - residual_scale == 0.f)) { set_error("residual_scale must be finite"); return DDIT_ERR_INVALID_ARG; }
+  if (D % 8) { set_error("D=%d must be a multiple of 8", D); return DDIT_ERR_UNSUPPORTED; }
+  if (D > 8192) { set_error("D=%d: more than 8192 features are not supported by the norms around a branch", D); return DDIT_ERR_UNSUPPORTED; }
+  if (N > (int64_t)1 << 40) { set_error("N=%lld tokens: too many", (long long)N); return DDIT_ERR_UNSUPPORTED; }
+  if (ld_f < D || (out_or_null && ld_out < D)) { set_error("leading dimensions (%lld,%lld) must be at least D=%d", (long long)ld_f, (long long)ld_out, D); return DDIT_ERR_INVALID_ARG; }
+  if (ld_f % 8 || (out_or_null && ld_out % 8)) { set_error("leading dimensions must be multiples of 8"); return DDIT_ERR_ALIGNMENT; }
+  if (gate_row >= 0 && (!gate_table || !c6)) { set_error("gate_row=%d needs gate_table and c6", gate_row); return DDIT_ERR_INVALID_ARG; }
+  if (which >= 0 && (!next_table || !c6)) { set_error("which=%d needs next_table and c6", which); return DDIT_ERR_INVALID_ARG; }
+  if (which >= 0 && !out_or_null) { set_error("which=%d modulates an output that is not given", which); return DDIT_ERR_INVALID_ARG; }
+  for (const void *q : {f, g_post_or_null, (const void *)x, (const void *)gate_table, (const void *)c6, (const void *)x_out, g_pre_or_null,
+                        (const void *)next_table, (const void *)out_or_null})
+    if (q && !aligned16(q)) { set_error("pointers must be 16-byte aligned"); return DDIT_ERR_ALIGNMENT; }
+  BranchNormsArgs a;
+  memset(&a, 0, sizeof(a));
+  a.norm = norm; a.f = f; a.ld_f = ld_f; a.g_post = g_post_or_null; a.g_pre = g_pre_or_null;
+  a.x = x; a.residual_scale = residual_scale; a.x_out = x_out;
+  if (gate_row >= 0) { a.gate_tab = gate_table + (int64_t)gate_row * D; a.gate_c6 = c6 + (int64_t)gate_row * D; }
+  if (which >= 0) { a.mod_tab = next_table + (int64_t)3 * which * D; a.mod_c6 = c6 + (int64_t)3 * which * D; }
+  a.N = N; a.tokens_per_sample = tokens_per_sample; a.D = D; a.eps = eps; a.out = out_or_null; a.ld_out = ld_out;
+  return launch_branch_norms(a, reinterpret_cast<hipStream_t>(hip_stream));
 }
 
 int ddit_linear_tile_count(void) { return gemm_tile_count(); }
