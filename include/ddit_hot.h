@@ -283,6 +283,35 @@ int ddit_branch_norms_fwd(int norm, const void *f, int64_t ld_f, const void *g_p
                           const float *next_table, int which, int64_t N, int64_t tokens_per_sample, int32_t D, float eps,
                           void *out_or_null, int64_t ld_out, void *hip_stream);
 
+/* Microscaled 4-bit floating point ("mx4"): 32 consecutive values along k share a scale 2^(byte - 127); a value is a sign bit (the
+ * highest of its four) and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 (codes 0..7) times that scale.  The scale byte of a block is
+ * max(E - 2, 0), E = the bf16 exponent field of its largest magnitude; values are rounded to nearest, ties to the even code, and
+ * saturate at 6.  A block that holds an Inf or a NaN gets the byte 255 and is NaN as a whole.
+ * Layout of rows x k values: P = ceil(k / 128) panels, behind one another; a panel is [rows, 64] bytes of codes (byte j of a row: value
+ * 128 panel + 2 j in the low half, 128 panel + 2 j + 1 in the high half) and, in an array of its own, [rows, 4] scale bytes.  Values
+ * past k are 0.  k is a multiple of 8; rows * P * 64 below 2^31.
+ * ddit_mx4_bytes: sizes of the two arrays (host only; needs no GPU).  ddit_mx4_quantize: x bf16 [rows,k], row stride ld_x, into them.
+ * ddit_mx4_dequantize: the values that they stand for, bf16 [rows,k] (exact), row stride ld_out. */
+int ddit_mx4_bytes(int64_t rows, int32_t k, size_t *code_bytes_out, size_t *scale_bytes_out);
+int ddit_mx4_quantize(const void *x, int64_t ld_x, int64_t rows, int32_t k, void *codes, void *scales, void *hip_stream);
+int ddit_mx4_dequantize(const void *codes, const void *scales, int64_t rows, int32_t k, void *out, int64_t ld_out, void *hip_stream);
+
+/* ddit_linear_fwd with both operands in mx4: out = Q(u) W^T + bias with the epilogues of ddit_linear_fwd, fp32 sums, except that the
+ * residual update reads resid and writes resid_out (fp32 [N,n]; they may be the same).  W_codes, W_scales: the weight [n,k] as
+ * ddit_mx4_quantize lays it out; bias bf16 [n] or NULL.  ddit_linear_mx4_fwd takes u bf16 [N,k] and quantises it on the way, in
+ * a workspace (256-byte aligned, ddit_linear_mx4_workspace_bytes(); free again when the call's work is done);
+ * ddit_linear_mx4_codes_fwd takes it quantised already, as by several linears that share u.  No output may overlap an input but
+ * resid_out resid.  N = 0 as above. */
+int ddit_linear_mx4_workspace_bytes(int64_t N, int32_t n, int32_t k, size_t *bytes_out);
+int ddit_linear_mx4_fwd(int epilogue, const void *u, int64_t ld_u, const void *W_codes, const void *W_scales, const void *bias, int64_t N,
+                        int32_t n, int32_t k, void *out, int64_t ld_out, const float *resid, float *resid_out, const float *ada_table,
+                        const float *c6, int gate_row, int64_t tokens_per_sample, void *workspace, size_t workspace_bytes,
+                        void *hip_stream);
+int ddit_linear_mx4_codes_fwd(int epilogue, const void *u_codes, const void *u_scales, const void *W_codes, const void *W_scales,
+                              const void *bias, int64_t N, int32_t n, int32_t k, void *out, int64_t ld_out, const float *resid,
+                              float *resid_out, const float *ada_table, const float *c6, int gate_row, int64_t tokens_per_sample,
+                              void *hip_stream);
+
 /* ---- output tiles of the linear: for tuning and for parity tests of every compiled tile ----
  * The linear is compiled for a short list of output tiles (rows x cols of out per workgroup), which callers can force, and for
  * a few forms beside the list.  ddit_linear_fwd takes, per call, a form for few tokens where its grid finds room on the device

@@ -34,7 +34,8 @@ EXPORTS = ["ddit_abi_version", "ddit_status_string", "ddit_last_error", "ddit_wo
            "ddit_linear_partial_choice", "ddit_linear_partial_fwd", "ddit_qk_norm_rope_fwd", "ddit_self_attn_fwd", "ddit_optimal_dop",
            "ddit_buddy_create", "ddit_buddy_alloc", "ddit_buddy_release", "ddit_buddy_free_gpus", "ddit_buddy_destroy",
            "ddit_sched_simulate", "ddit_probe_mfma_bf16", "ddit_probe_stream_copy", "ddit_probe_stream_read", "ddit_probe_residual_stream",
-           "ddit_branch_norms_fwd"]
+           "ddit_branch_norms_fwd", "ddit_mx4_bytes", "ddit_mx4_quantize", "ddit_mx4_dequantize", "ddit_linear_mx4_workspace_bytes",
+           "ddit_linear_mx4_fwd", "ddit_linear_mx4_codes_fwd"]
 
 
 class ddit_shape(C.Structure):
@@ -177,6 +178,13 @@ def _load() -> C.CDLL:
     lib.ddit_probe_residual_stream.argtypes = [VP, VP, VP, VP, C.c_int64, C.c_int32, C.c_int32, VP]
     lib.ddit_branch_norms_fwd.argtypes = [C.c_int, VP, C.c_int64, VP, VP, C.c_float, VP, VP, C.c_int, VP, VP, VP, C.c_int, C.c_int64,
                                           C.c_int64, C.c_int32, C.c_float, VP, C.c_int64, VP]
+    I64, I32, SZ = C.c_int64, C.c_int32, C.c_size_t
+    lib.ddit_mx4_bytes.argtypes = [I64, I32, C.POINTER(SZ), C.POINTER(SZ)]
+    lib.ddit_mx4_quantize.argtypes = [VP, I64, I64, I32, VP, VP, VP]
+    lib.ddit_mx4_dequantize.argtypes = [VP, VP, I64, I32, VP, I64, VP]
+    lib.ddit_linear_mx4_workspace_bytes.argtypes = [I64, I32, I32, C.POINTER(SZ)]
+    lib.ddit_linear_mx4_fwd.argtypes = [C.c_int, VP, I64, VP, VP, VP, I64, I32, I32, VP, I64, VP, VP, VP, VP, C.c_int, I64, VP, SZ, VP]
+    lib.ddit_linear_mx4_codes_fwd.argtypes = [C.c_int, VP, VP, VP, VP, VP, I64, I32, I32, VP, I64, VP, VP, VP, VP, C.c_int, I64, VP]
     for n in EXPORTS:
         if n not in ("ddit_abi_version", "ddit_status_string", "ddit_last_error", "ddit_linear_tile_count"):
             getattr(lib, n).restype = C.c_int
@@ -534,6 +542,40 @@ def ddit_branch_norms_fwd(norm: int, f, ld_f: int, g_post, x, residual_scale: fl
     _check(_lib.ddit_branch_norms_fwd(norm, _ptr(f), ld_f, _ptr(g_post), _ptr(x), residual_scale, _ptr(gate_table), _ptr(c6), gate_row,
                                       _ptr(x_out), _ptr(g_pre), _ptr(next_table), which, N, tokens_per_sample, D, eps, _ptr(out), ld_out,
                                       _stream()))
+
+
+def ddit_mx4_bytes(rows: int, k: int):
+    """-> (bytes of the codes, bytes of the scales)."""
+    c, s = C.c_size_t(0), C.c_size_t(0)
+    _check(_lib.ddit_mx4_bytes(rows, k, C.byref(c), C.byref(s)))
+    return int(c.value), int(s.value)
+
+
+def ddit_mx4_quantize(x, ld_x: int, rows: int, k: int, codes, scales) -> None:
+    _check(_lib.ddit_mx4_quantize(_ptr(x), ld_x, rows, k, _ptr(codes), _ptr(scales), _stream()))
+
+
+def ddit_mx4_dequantize(codes, scales, rows: int, k: int, out, ld_out: int) -> None:
+    _check(_lib.ddit_mx4_dequantize(_ptr(codes), _ptr(scales), rows, k, _ptr(out), ld_out, _stream()))
+
+
+def ddit_linear_mx4_workspace_bytes(N: int, n: int, k: int) -> int:
+    b = C.c_size_t(0)
+    _check(_lib.ddit_linear_mx4_workspace_bytes(N, n, k, C.byref(b)))
+    return int(b.value)
+
+
+def ddit_linear_mx4_fwd(epilogue: int, u, ld_u: int, W_codes, W_scales, bias, N: int, n: int, k: int, out, ld_out: int, workspace, resid=None,
+                        resid_out=None, ada_table=None, c6=None, gate_row: int = -1, tokens_per_sample: int = 1) -> None:
+    _check(_lib.ddit_linear_mx4_fwd(epilogue, _ptr(u), ld_u, _ptr(W_codes), _ptr(W_scales), _ptr(bias), N, n, k, _ptr(out), ld_out, _ptr(resid),
+                                    _ptr(resid_out), _ptr(ada_table), _ptr(c6), gate_row, tokens_per_sample, _ptr(workspace),
+                                    _nbytes(workspace), _stream()))
+
+
+def ddit_linear_mx4_codes_fwd(epilogue: int, u_codes, u_scales, W_codes, W_scales, bias, N: int, n: int, k: int, out, ld_out: int, resid=None,
+                              resid_out=None, ada_table=None, c6=None, gate_row: int = -1, tokens_per_sample: int = 1) -> None:
+    _check(_lib.ddit_linear_mx4_codes_fwd(epilogue, _ptr(u_codes), _ptr(u_scales), _ptr(W_codes), _ptr(W_scales), _ptr(bias), N, n, k, _ptr(out),
+                                          ld_out, _ptr(resid), _ptr(resid_out), _ptr(ada_table), _ptr(c6), gate_row, tokens_per_sample, _stream()))
 
 
 def ddit_probe_mfma_bf16(operands, sink, iters: int) -> float:

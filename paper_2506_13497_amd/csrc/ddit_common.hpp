@@ -26,6 +26,14 @@ __device__ __forceinline__ floatx16 mfma32(bf16x8 a, bf16x8 b, floatx16 c) {
 
 __device__ __forceinline__ float bf16_bits_to_float(uint16_t b) { return __uint_as_float(((uint32_t)b) << 16); }
 
+__device__ __forceinline__ float gelu_tanh_f(float u) {
+  // 0.5 u (1 + tanh(z)) == u / (1 + exp(-2 z)),  z = sqrt(2/pi) (u + 0.044715 u^3)
+  const float kA = -2.0f * 0.7978845608028654f * 1.4426950408889634f;  // -2 sqrt(2/pi) log2(e)
+  const float t = u * u;
+  const float z2 = u * (kA + (kA * 0.044715f) * t);                    // -2 z log2(e)
+  return u * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z2));
+}
+
 __device__ __forceinline__ float wave_sum(float v) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
@@ -192,6 +200,22 @@ struct BranchNormsArgs {
   void *out; int64_t ld_out;           // bf16 [N, D] or null
 };
 int launch_branch_norms(const BranchNormsArgs &a, hipStream_t s);
+
+// microscaled 4-bit floating point (mx4.hip): panels of 128 of k, codes [panels][rows][64] bytes, scales [panels][rows][4] bytes
+inline int64_t mx4_panels(int64_t k) { return (k + 127) / 128; }
+int launch_mx4_quantize(const void *x, int64_t ld_x, int64_t rows, int k, void *codes, void *scales, hipStream_t s);
+int launch_mx4_dequantize(const void *codes, const void *scales, int64_t rows, int k, void *out, int64_t ld_out, hipStream_t s);
+struct Mx4GemmArgs {
+  const void *u_codes, *u_scales;     // [N, k] quantised
+  const void *w_codes, *w_scales;     // [n, k] quantised
+  const void *bias;                   // bf16 [n] or null
+  int64_t N; int n; int k;
+  void *out; int64_t ld_out;          // bf16 [N, n] (may be null for the residual update)
+  const float *resid; float *resid_out;   // fp32 [N, n]; may be the same
+  const float *gate_tab, *gate_c6; int64_t gate_c6_stride;   // as in GemmArgs
+  int64_t tokens_per_sample;
+};
+int launch_mx4_gemm(int epilogue, const Mx4GemmArgs &a, hipStream_t s);
 
 // layers around the token-space step, solver
 int launch_position_code(float *pos, int Hp, int Wp, int D, hipStream_t s);

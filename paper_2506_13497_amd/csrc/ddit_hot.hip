@@ -899,6 +899,114 @@ int ddit_branch_norms_fwd(int norm, const void *f, int64_t ld_f, const void *g_p
   return launch_branch_norms(a, reinterpret_cast<hipStream_t>(hip_stream));
 }
 
+// rows x k values in four bits: the panels' bytes have to stay below 2^31, which the product indexes with 32 bits
+static int check_mx4(int64_t rows, int32_t k, const char *what) {
+  if (rows < 0 || k < 1) { set_error("mx4: %s=%lld k=%d", what, (long long)rows, k); return DDIT_ERR_INVALID_ARG; }
+  if (k % 8) { set_error("mx4: k=%d must be a multiple of 8", k); return DDIT_ERR_UNSUPPORTED; }
+  if (rows > (((int64_t)1 << 31) - 1) / (mx4_panels(k) * 64)) {
+    set_error("mx4: %s=%lld rows of k=%d exceed the 31-bit byte range of the codes", what, (long long)rows, k); return DDIT_ERR_UNSUPPORTED;
+  }
+  return DDIT_OK;
+}
+
+int ddit_mx4_bytes(int64_t rows, int32_t k, size_t *code_bytes_out, size_t *scale_bytes_out) {
+  DDIT_TRY(check_mx4(rows, k, "rows"));
+  if (!code_bytes_out || !scale_bytes_out) { set_error("code_bytes_out and scale_bytes_out must not be NULL"); return DDIT_ERR_INVALID_ARG; }
+  *code_bytes_out = (size_t)rows * mx4_panels(k) * 64;
+  *scale_bytes_out = (size_t)rows * mx4_panels(k) * 4;
+  return DDIT_OK;
+}
+
+static int check_mx4_copy(const void *dense, int64_t ld, int64_t rows, int32_t k, const void *codes, const void *scales) {
+  DDIT_TRY(check_mx4(rows, k, "rows"));
+  if (!dense || !codes || !scales) { set_error("the values, codes and scales must not be NULL"); return DDIT_ERR_INVALID_ARG; }
+  if (ld < k) { set_error("leading dimension %lld below k=%d", (long long)ld, k); return DDIT_ERR_INVALID_ARG; }
+  if (ld % 8 || !aligned16(dense) || !aligned16(codes) || !aligned16(scales)) {
+    set_error("pointers must be 16-byte aligned and leading dimensions multiples of 8"); return DDIT_ERR_ALIGNMENT;
+  }
+  return DDIT_OK;
+}
+
+int ddit_mx4_quantize(const void *x, int64_t ld_x, int64_t rows, int32_t k, void *codes, void *scales, void *hip_stream) {
+  DDIT_TRY(check_mx4_copy(x, ld_x, rows, k, codes, scales));
+  return launch_mx4_quantize(x, ld_x, rows, k, codes, scales, reinterpret_cast<hipStream_t>(hip_stream));
+}
+
+int ddit_mx4_dequantize(const void *codes, const void *scales, int64_t rows, int32_t k, void *out, int64_t ld_out, void *hip_stream) {
+  DDIT_TRY(check_mx4_copy(out, ld_out, rows, k, codes, scales));
+  return launch_mx4_dequantize(codes, scales, rows, k, out, ld_out, reinterpret_cast<hipStream_t>(hip_stream));
+}
+
+int ddit_linear_mx4_workspace_bytes(int64_t N, int32_t n, int32_t k, size_t *bytes_out) {
+  DDIT_TRY(check_mx4(N, k, "N"));
+  if (n < 1) { set_error("linear: n=%d", n); return DDIT_ERR_INVALID_ARG; }
+  if (!bytes_out) { set_error("bytes_out is NULL"); return DDIT_ERR_INVALID_ARG; }
+  *bytes_out = align_up((size_t)N * mx4_panels(k) * 64) + align_up((size_t)N * mx4_panels(k) * 4);
+  return DDIT_OK;
+}
+
+// the arguments that the two linears share, into *g
+static int check_linear_mx4(int epilogue, const void *W_codes, const void *W_scales, const void *bias, int64_t N, int32_t n, int32_t k, void *out,
+                            int64_t ld_out, const float *resid, float *resid_out, const float *ada_table, const float *c6, int gate_row,
+                            int64_t tokens_per_sample, Mx4GemmArgs *g) {
+  if (epilogue < 0 || epilogue > 2) { set_error("unknown epilogue %d", epilogue); return DDIT_ERR_INVALID_ARG; }
+  if (!W_codes || !W_scales) { set_error("W_codes and W_scales must not be NULL"); return DDIT_ERR_INVALID_ARG; }
+  if (n < 1) { set_error("linear: n=%d", n); return DDIT_ERR_INVALID_ARG; }
+  DDIT_TRY(check_mx4(N, k, "N"));
+  DDIT_TRY(check_mx4(n, k, "n"));
+  if (n % 8) { set_error("n=%d must be a multiple of 8", n); return DDIT_ERR_UNSUPPORTED; }
+  memset(g, 0, sizeof(*g));
+  if (epilogue == DDIT_EPI_RESIDUAL_F32) {
+    if (!resid || !resid_out) { set_error("resid and resid_out must not be NULL for the residual epilogue"); return DDIT_ERR_INVALID_ARG; }
+    if (gate_row >= 0) {
+      if (gate_row > 5 || !ada_table || !c6) { set_error("gate_row=%d needs ada_table and c6, and must be < 6", gate_row); return DDIT_ERR_INVALID_ARG; }
+      if (tokens_per_sample < 1) { set_error("tokens_per_sample=%lld", (long long)tokens_per_sample); return DDIT_ERR_INVALID_ARG; }
+      g->gate_tab = ada_table + (int64_t)gate_row * n;
+      g->gate_c6 = c6 + (int64_t)gate_row * n;
+      g->gate_c6_stride = 6 * (int64_t)n;
+    }
+  } else if (!out) {
+    set_error("out must not be NULL"); return DDIT_ERR_INVALID_ARG;
+  }
+  if (out && ld_out < n) { set_error("ld_out=%lld below n=%d", (long long)ld_out, n); return DDIT_ERR_INVALID_ARG; }
+  if (out && ld_out % 8) { set_error("ld_out=%lld must be a multiple of 8", (long long)ld_out); return DDIT_ERR_ALIGNMENT; }
+  for (const void *q : {W_codes, W_scales, bias, (const void *)out, (const void *)resid, (const void *)resid_out, (const void *)ada_table, (const void *)c6})
+    if (q && !aligned16(q)) { set_error("pointers must be 16-byte aligned"); return DDIT_ERR_ALIGNMENT; }
+  g->w_codes = W_codes; g->w_scales = W_scales; g->bias = bias; g->N = N; g->n = n; g->k = k; g->out = out; g->ld_out = ld_out;
+  g->resid = resid; g->resid_out = resid_out; g->tokens_per_sample = tokens_per_sample > 0 ? tokens_per_sample : 1;
+  return DDIT_OK;
+}
+
+int ddit_linear_mx4_codes_fwd(int epilogue, const void *u_codes, const void *u_scales, const void *W_codes, const void *W_scales, const void *bias,
+                              int64_t N, int32_t n, int32_t k, void *out, int64_t ld_out, const float *resid, float *resid_out,
+                              const float *ada_table, const float *c6, int gate_row, int64_t tokens_per_sample, void *hip_stream) {
+  Mx4GemmArgs g;
+  if (!u_codes || !u_scales) { set_error("u_codes and u_scales must not be NULL"); return DDIT_ERR_INVALID_ARG; }
+  DDIT_TRY(check_linear_mx4(epilogue, W_codes, W_scales, bias, N, n, k, out, ld_out, resid, resid_out, ada_table, c6, gate_row, tokens_per_sample, &g));
+  if (!aligned16(u_codes) || !aligned16(u_scales)) { set_error("pointers must be 16-byte aligned"); return DDIT_ERR_ALIGNMENT; }
+  g.u_codes = u_codes; g.u_scales = u_scales;
+  return launch_mx4_gemm(epilogue, g, reinterpret_cast<hipStream_t>(hip_stream));
+}
+
+int ddit_linear_mx4_fwd(int epilogue, const void *u, int64_t ld_u, const void *W_codes, const void *W_scales, const void *bias, int64_t N,
+                        int32_t n, int32_t k, void *out, int64_t ld_out, const float *resid, float *resid_out, const float *ada_table,
+                        const float *c6, int gate_row, int64_t tokens_per_sample, void *workspace, size_t workspace_bytes, void *hip_stream) {
+  Mx4GemmArgs g;
+  if (!u) { set_error("u must not be NULL"); return DDIT_ERR_INVALID_ARG; }
+  DDIT_TRY(check_linear_mx4(epilogue, W_codes, W_scales, bias, N, n, k, out, ld_out, resid, resid_out, ada_table, c6, gate_row, tokens_per_sample, &g));
+  if (ld_u < k) { set_error("linear: ld_u=%lld below k=%d", (long long)ld_u, k); return DDIT_ERR_INVALID_ARG; }
+  if (ld_u % 8 || !aligned16(u)) { set_error("u must be 16-byte aligned and ld_u a multiple of 8"); return DDIT_ERR_ALIGNMENT; }
+  if (N == 0) return DDIT_OK;
+  size_t need = 0;
+  DDIT_TRY(ddit_linear_mx4_workspace_bytes(N, n, k, &need));
+  DDIT_TRY(check_ws(workspace, workspace_bytes, need));
+  unsigned char *ws = reinterpret_cast<unsigned char *>(workspace);
+  g.u_codes = ws; g.u_scales = ws + align_up((size_t)N * mx4_panels(k) * 64);
+  hipStream_t s = reinterpret_cast<hipStream_t>(hip_stream);
+  DDIT_TRY(launch_mx4_quantize(u, ld_u, N, k, ws, const_cast<void *>(g.u_scales), s));
+  return launch_mx4_gemm(epilogue, g, s);
+}
+
 int ddit_linear_tile_count(void) { return gemm_tile_count(); }
 
 int ddit_linear_tile_info(int tile, int32_t *rows, int32_t *cols, int32_t *wavefronts, int32_t *workgroups_per_cu) {

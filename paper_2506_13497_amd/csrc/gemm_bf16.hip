@@ -83,14 +83,6 @@ struct GroupTable {
 };
 struct NoGroups {};
 
-__device__ __forceinline__ float gelu_tanh_f(float u) {
-  // 0.5 u (1 + tanh(z)) == u / (1 + exp(-2 z)),  z = sqrt(2/pi) (u + 0.044715 u^3)
-  const float kA = -2.0f * 0.7978845608028654f * 1.4426950408889634f;  // -2 sqrt(2/pi) log2(e)
-  const float t = u * u;
-  const float z2 = u * (kA + (kA * 0.044715f) * t);                    // -2 z log2(e)
-  return u * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z2));
-}
-
 // Workgroup barrier that orders LDS traffic only.  __syncthreads() would also wait for the
 // epilogue's global stores of the previous tile to be acknowledged; nothing in this kernel
 // communicates through global memory inside a workgroup.

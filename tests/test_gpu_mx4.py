@@ -1,0 +1,274 @@
+"""Microscaled 4-bit floating point: the quantiser against its definition in float64 (bit for bit), its inverse, and the linears against
+float64 products of the values that the codes stand for.
+
+Tolerance of the product: its terms are products of two values of four bits and powers of two, exact in fp32.  P panels are summed in
+at most 3 additions a panel of one chain, joined with at most 16 others, each off by 2^-24 of the partial sum, which is at most
+A = |Q(u)| |W|^T + |b|: (4 P + 20) 2^-24 A.  bf16 rounds by 2^-8 of the value; GELU's slope is at most 1.13 and its own arithmetic 16 units
+of 2^-24 of |y| (+ 2^-24 for what the exponential leaves near zero)."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+GRID = torch.tensor([0, 0.5, 1, 1.5, 2, 3, 4, 6, -0.0, -0.5, -1, -1.5, -2, -3, -4, -6], dtype=torch.float64)
+
+
+@pytest.fixture(scope="module")
+def m():
+    import paper_2506_13497_amd as mod
+    return mod
+
+
+def encode64(x):
+    """bf16 [rows, k] on the CPU -> codes [panels, rows, 64], scales [panels, rows, 4], by the definition."""
+    rows, k = x.shape
+    P = (k + 127) // 128
+    v = torch.zeros((rows, P * 128), dtype=torch.float64)
+    v[:, :k] = x.double()
+    bits = torch.zeros((rows, P * 128), dtype=torch.int64)
+    bits[:, :k] = x.contiguous().view(torch.int16).long() & 0x7fff
+    field = (bits.view(rows, -1, 32).amax(2)) >> 7
+    byte = torch.where(field == 255, torch.full_like(field, 255), (field - 2).clamp(min=0))
+    y = v.view(rows, -1, 32) * torch.pow(2.0, 127.0 - byte.double())[..., None]
+    a = y.abs().nan_to_num(0.0, 0.0)
+    code = torch.zeros(a.shape, dtype=torch.int64)
+    for i, border in enumerate((0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0)):
+        code += (a >= border) if i % 2 else (a > border)
+    code |= torch.signbit(y).long() << 3
+    code = torch.where((byte == 255)[..., None], torch.zeros_like(code), code).view(rows, P, 64, 2)
+    codes = (code[..., 0] | code[..., 1] << 4).to(torch.uint8).permute(1, 0, 2).contiguous()
+    return codes, byte.view(rows, P, 4).to(torch.uint8).permute(1, 0, 2).contiguous()
+
+
+def decode64(codes, scales, k):
+    P, rows, _ = codes.shape
+    c = codes.permute(1, 0, 2).long()
+    v = GRID.to(codes.device)[torch.stack((c & 15, c >> 4), -1)].view(rows, P * 4, 32)
+    s = scales.permute(1, 0, 2).reshape(rows, P * 4).long()
+    f = torch.where(s == 255, torch.full(s.shape, math.nan, dtype=torch.float64, device=s.device), torch.pow(2.0, s.double() - 127))
+    return (v * f[..., None]).view(rows, P * 128)[:, :k]
+
+
+def _arrays(m, rows, k, guard=64):
+    """-> codes and scales as views in front of guard bytes"""
+    cb, sb = m.ddit_mx4_bytes(rows, k)
+    P = (k + 127) // 128
+    assert (cb, sb) == (P * rows * 64, P * rows * 4)
+    c = torch.full((cb + guard,), 0xA5, dtype=torch.uint8, device="cuda")
+    s = torch.full((sb + guard,), 0xA5, dtype=torch.uint8, device="cuda")
+    return c, s, c[:cb].view(P, rows, 64), s[:sb].view(P, rows, 4)
+
+
+def _same_values(a, b):
+    return torch.equal(a.view(torch.int16), b.view(torch.int16))
+
+
+@pytest.mark.parametrize("rows,k,ld", [(1, 8, 8), (1, 128, 128), (3, 72, 80), (5, 1152, 1152), (16, 136, 136), (63, 32, 64), (65, 264, 264), (300, 1160, 2304),
+                                       (1000, 4608, 4608)])
+def test_quantiser_bit_for_bit(m, rows, k, ld):
+    g = torch.Generator().manual_seed(rows + k)
+    x = torch.randn((rows, ld), generator=g) * torch.exp(2 * torch.randn((1, ld), generator=g)) * torch.exp(4 * torch.randn((rows, 1), generator=g))
+    x = x.bfloat16()
+    x[:, k:] = float("nan")                       # between the rows: not read
+    x[rows // 2, : min(k, 32)] = 0
+    xd = x.cuda()
+    call, sall, codes, scales = _arrays(m, rows, k)
+    m.ddit_mx4_quantize(xd, ld, rows, k, codes, scales)
+    out = torch.full((rows, ld), -7.0, dtype=torch.bfloat16, device="cuda")
+    m.ddit_mx4_dequantize(codes, scales, rows, k, out, ld)
+    torch.cuda.synchronize()
+    want_c, want_s = encode64(x[:, :k])
+    assert torch.equal(codes.cpu(), want_c) and torch.equal(scales.cpu(), want_s)
+    assert (call[codes.numel():] == 0xA5).all() and (sall[scales.numel():] == 0xA5).all()
+    assert torch.equal(out[:, :k].cpu().double(), decode64(want_c, want_s, k)) and (out[:, k:] == -7).all()
+
+
+def test_every_bf16_value_at_every_scale(m):
+    """Blocks of one large value, which fixes the scale, and others: all bf16 bit patterns below it."""
+    every = torch.from_numpy(np.arange(65536, dtype=np.uint16).view(np.int16).copy()).view(torch.bfloat16)
+    for field in (0, 1, 2, 3, 100, 127, 128, 254):
+        top = torch.tensor([max(field << 7, 1) | 0x55 if field else 0x7f], dtype=torch.int16).view(torch.bfloat16)
+        below = every[(every.view(torch.int16).int() & 0x7fff) < ((field + 1) << 7)]
+        below = below[: below.numel() // 31 * 31].view(-1, 31)
+        x = torch.cat((top.expand(below.shape[0], 1), below), 1).contiguous()
+        _, _, codes, scales = _arrays(m, x.shape[0], 32)
+        out = torch.empty((x.shape[0], 32), dtype=torch.bfloat16, device="cuda")
+        m.ddit_mx4_quantize(x.cuda(), 32, x.shape[0], 32, codes, scales)
+        m.ddit_mx4_dequantize(codes, scales, x.shape[0], 32, out, 32)
+        torch.cuda.synchronize()
+        want_c, want_s = encode64(x)
+        assert torch.equal(codes.cpu(), want_c) and torch.equal(scales.cpu(), want_s), field
+        assert torch.equal(out.cpu().double(), decode64(want_c, want_s, 32)), field
+
+
+def test_blocks_with_inf_and_nan(m):
+    x = torch.ones((4, 96), dtype=torch.bfloat16)
+    x[0, 3], x[1, 40], x[2, 95], x[3, 31] = math.inf, -math.inf, math.nan, 3.3895e38
+    _, _, codes, scales = _arrays(m, 4, 96)
+    out = torch.empty((4, 96), dtype=torch.bfloat16, device="cuda")
+    m.ddit_mx4_quantize(x.cuda(), 96, 4, 96, codes, scales)
+    m.ddit_mx4_dequantize(codes, scales, 4, 96, out, 96)
+    torch.cuda.synchronize()
+    bad = torch.zeros((4, 3), dtype=torch.bool)
+    bad[0, 0] = bad[1, 1] = bad[2, 2] = True
+    assert torch.equal(out.cpu().view(4, 3, 32).isnan().all(2), bad) and torch.equal(out.cpu().view(4, 3, 32).isnan().any(2), bad)
+    want_c, want_s = encode64(x)
+    assert torch.equal(codes.cpu(), want_c) and torch.equal(scales.cpu(), want_s)
+
+
+# ------------------------------------------------------------------------------------------------ linears
+def _problem(m, N, n, k, seed, ld_u=None, gain=1.0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    draw = lambda *s: torch.randn(*s, device="cuda", generator=g)
+    ld_u = ld_u or k
+    u = torch.full((N, ld_u), float("nan"), device="cuda")
+    u[:, :k] = draw(N, k) * torch.exp(0.7 * draw(1, k)) * gain
+    t = dict(u=u.bfloat16(), bias=(0.3 * draw(n)).bfloat16(), x=3 * draw(N, n), table=0.5 * draw(6, n))
+    W = (0.05 * draw(n, k)).bfloat16()
+    _, _, t["wc"], t["ws"] = _arrays(m, n, k)
+    m.ddit_mx4_quantize(W, k, n, k, t["wc"], t["ws"])
+    _, _, t["uc"], t["us"] = _arrays(m, N, k)
+    m.ddit_mx4_quantize(t["u"], ld_u, N, k, t["uc"], t["us"])
+    torch.cuda.synchronize()
+    t["c6"] = lambda tps: 0.5 * draw((N + tps - 1) // tps, 6 * n)
+    t["W64"], t["u64"] = decode64(t["wc"], t["ws"], k), decode64(t["uc"], t["us"], k)
+    return t
+
+
+def _linear64(t, k, bias):
+    y, A = t["u64"] @ t["W64"].t().contiguous(), t["u64"].abs() @ t["W64"].abs().t().contiguous()
+    if bias:
+        y, A = y + t["bias"].double(), A + t["bias"].double().abs()
+    return y, (4 * ((k + 127) // 128) + 20) * U * A
+
+
+def _check_linear(m, N, n, k, epi, seed=1, bias=True, tps=None, gate_row=5, ld_out=None, ld_u=None, codes=False, copy=True):
+    tps = tps or N
+    t = _problem(m, N, n, k, seed, ld_u)
+    y, e = _linear64(t, k, bias)
+    ld_out = ld_out or n
+    out = torch.full((N + 2, ld_out), -7.0, dtype=torch.bfloat16, device="cuda")
+    x_out = torch.full((N + 2, n), -7.0, device="cuda")
+    kw = {}
+    if epi == m.DDIT_EPI_RESIDUAL_F32:
+        c6 = t["c6"](tps)
+        kw = dict(resid=t["x"], resid_out=x_out, ada_table=t["table"], c6=c6, gate_row=gate_row, tokens_per_sample=tps)
+    o = out if copy else None
+    b = t["bias"] if bias else None
+    if codes:
+        m.ddit_linear_mx4_codes_fwd(epi, t["uc"], t["us"], t["wc"], t["ws"], b, N, n, k, o, ld_out, **kw)
+    else:
+        ws = torch.full((m.ddit_linear_mx4_workspace_bytes(N, n, k),), 0xFF, dtype=torch.uint8, device="cuda")
+        m.ddit_linear_mx4_fwd(epi, t["u"], ld_u or k, t["wc"], t["ws"], b, N, n, k, o, ld_out, ws, **kw)
+    torch.cuda.synchronize()
+    if epi == m.DDIT_EPI_GELU_BF16:
+        z = math.sqrt(2 / math.pi) * (y + 0.044715 * y ** 3)
+        e = 1.13 * e + 16 * U * y.abs() + U
+        y = 0.5 * y * (1 + torch.tanh(z))
+    if epi == m.DDIT_EPI_RESIDUAL_F32:
+        gate = 1.0
+        if gate_row >= 0:
+            at = torch.arange(N, device="cuda") // tps
+            gate = (t["table"].double()[gate_row] + c6.double().view(-1, 6, n)[at, gate_row])
+            e = gate.abs() * (e + 2 * U * y.abs())
+        y = t["x"].double() + gate * y
+        e = e + 2 * U * y.abs()
+        assert ((x_out[:N].double() - y).abs() <= e).all() and (x_out[N:] == -7).all()
+    if o is not None:
+        assert ((out[:N, :n].double() - y).abs() <= e + 2.0 ** -8 * (y.abs() + e)).all()
+    assert (out[N:] == -7).all() and (out[:, n:] == -7).all()
+    return out, x_out
+
+
+SIZES = [(1, 8, 8), (1, 64, 128), (1, 6912, 1152), (2, 1152, 4608), (7, 72, 40), (16, 1160, 136), (17, 200, 1160), (31, 136, 4608), (33, 1152, 1152), (64, 64, 64),
+         (65, 328, 264), (129, 2304, 1152), (300, 2304, 1152), (257, 264, 8192), (1000, 456, 520), (2304, 1152, 4608), (2305, 1160, 136), (6500, 2312, 392)]
+
+
+@pytest.mark.parametrize("N,n,k", SIZES)
+@pytest.mark.parametrize("epi", [0, 1, 2])
+def test_linear(m, N, n, k, epi):
+    _check_linear(m, N, n, k, epi, seed=N + n + k)
+
+
+@pytest.mark.parametrize("epi", [0, 2])
+@pytest.mark.parametrize("N", [3, 48, 700, 5000])
+def test_linear_options(m, N, epi):
+    _check_linear(m, N, 392, 264, epi, bias=False, gate_row=-1, ld_u=272, ld_out=400)
+    _check_linear(m, N, 392, 264, epi, tps=max(1, N // 3), gate_row=0, copy=epi == 0)
+    a = _check_linear(m, N, 392, 264, epi, seed=4, tps=max(1, N // 3))
+    b = _check_linear(m, N, 392, 264, epi, seed=4, tps=max(1, N // 3), codes=True)
+    assert _same_values(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+def test_residual_in_place_and_long_products_of_many_tokens(m):
+    N, n, k = 9000, 1152, 4608
+    a = _check_linear(m, N, n, k, 2, seed=6, tps=2000)
+    t = _problem(m, N, n, k, 6)
+    c6 = t["c6"](2000)
+    x, out = t["x"].clone(), torch.empty((N, n), dtype=torch.bfloat16, device="cuda")
+    ws = torch.empty(m.ddit_linear_mx4_workspace_bytes(N, n, k), dtype=torch.uint8, device="cuda")
+    m.ddit_linear_mx4_fwd(2, t["u"], k, t["wc"], t["ws"], t["bias"], N, n, k, out, n, ws, resid=x, resid_out=x, ada_table=t["table"], c6=c6, gate_row=5,
+                          tokens_per_sample=2000)
+    torch.cuda.synchronize()
+    assert torch.equal(x, a[1][:N]) and _same_values(out, a[0][:N])
+
+
+@pytest.mark.parametrize("N", [1, 20, 400, 6000])
+def test_a_nan_stays_in_its_row(m, N):
+    """A token or a feature whose block is NaN makes its own row or column NaN and leaves every other as it was."""
+    n, k = 200, 328
+    t = _problem(m, N, n, k, 8)
+    out = [torch.empty((N, n), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    ws = torch.empty(m.ddit_linear_mx4_workspace_bytes(N, n, k), dtype=torch.uint8, device="cuda")
+    call = lambda o: m.ddit_linear_mx4_fwd(0, t["u"], k, t["wc"], t["ws"], t["bias"], N, n, k, o, n, ws)
+    call(out[0])
+    t["u"][N // 2, k - 1] = math.inf
+    t["ws"][1, 100, 2] = 255
+    call(out[1])
+    torch.cuda.synchronize()
+    row = torch.arange(N, device="cuda")[:, None] == N // 2
+    col = torch.arange(n, device="cuda")[None] == 100
+    assert torch.equal(out[1].isnan(), (row | col).expand(N, n))
+    assert torch.equal(out[1].masked_fill(row | col, 0), out[0].masked_fill(row | col, 0))
+
+
+def test_scales_far_apart(m):
+    """Rows whose scales sit at both ends of the range: products that leave fp32 are infinite or zero, as in float64 rounded to fp32."""
+    N, n, k = 40, 64, 128
+    t = _problem(m, N, n, k, 9)
+    us, ws = t["us"], t["ws"]
+    us[:, 0::4], us[:, 1::4], us[:, 2::4], us[:, 3::4] = 0, 60, 200, 252
+    ws[:, 0::2], ws[:, 1::2] = 1, 90
+    out = torch.empty((N, n), dtype=torch.bfloat16, device="cuda")
+    m.ddit_linear_mx4_codes_fwd(0, t["uc"], us, t["wc"], ws, None, N, n, k, out, n)
+    torch.cuda.synchronize()
+    u64, W64 = decode64(t["uc"], us, k), decode64(t["wc"], ws, k)
+    y, A = u64 @ W64.t().contiguous(), u64.abs() @ W64.abs().t().contiguous()
+    # 2^-126 is where fp32 may stop: products below it may be dropped, at most k of them
+    assert ((out.double() - y).abs() <= 24 * U * A + 2.0 ** -8 * y.abs() + k * 2.0 ** -126).all()
+
+
+@pytest.mark.parametrize("N", [2, 200, 5000])
+def test_captured_and_on_another_stream(m, N):
+    n, k = 1152, 1160
+    t = _problem(m, N, n, k, 10)
+    out, ws = torch.empty((N, n), dtype=torch.bfloat16, device="cuda"), torch.empty(m.ddit_linear_mx4_workspace_bytes(N, n, k), dtype=torch.uint8, device="cuda")
+    call = lambda o, w: m.ddit_linear_mx4_fwd(1, t["u"], k, t["wc"], t["ws"], t["bias"], N, n, k, o, n, w)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        call(out, ws)
+    torch.cuda.current_stream().wait_stream(s)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(out, ws)
+    other, ws2 = torch.empty_like(out), torch.empty_like(ws)
+    for seed in (1, 2, 3):
+        t["u"].copy_(torch.randn(N, k, device="cuda", generator=torch.Generator(device="cuda").manual_seed(seed)))
+        graph.replay()
+        call(other, ws2)
+        torch.cuda.synchronize()
+        assert _same_values(out, other)

@@ -40,3 +40,56 @@ def test_branch_norms_refusals(m):
     for bad in (dict(ld_f=68), dict(ld_out=68), dict(f=P(0x1008)), dict(x=P(0x2004)), dict(x_out=P(0x5008)), dict(g_post=P(0x8)), dict(g_pre=P(0x8)),
                 dict(gate_table=P(0x3004)), dict(c6=P(0x4008)), dict(next_table=P(0x6008)), dict(out=P(0x7008))):
         assert call(**bad) == -4, bad
+
+
+def test_mx4_sizes_and_refusals(m):
+    lib = m.binding._lib
+    assert m.ddit_mx4_bytes(0, 8) == (0, 0) and m.ddit_mx4_bytes(3, 8) == (192, 12) and m.ddit_mx4_bytes(5, 1152) == (5 * 9 * 64, 5 * 9 * 4)
+    assert m.ddit_mx4_bytes(5, 1160) == (5 * 10 * 64, 5 * 10 * 4)
+    assert m.ddit_linear_mx4_workspace_bytes(0, 64, 64) == 0
+    for N, n, k in [(1, 8, 8), (300, 2304, 1152), (48600, 1152, 4608)]:
+        c, s = m.ddit_mx4_bytes(N, k)
+        assert c + s <= m.ddit_linear_mx4_workspace_bytes(N, n, k) <= c + s + 512
+    size = C.c_size_t()
+    for rows, k, code in [(-1, 64, -1), (1, 0, -1), (1, 12, -2), (1 << 25, 128, -2), ((1 << 31), 8, -2), (1 << 62, 1 << 30, -2)]:
+        assert lib.ddit_mx4_bytes(rows, k, C.byref(size), C.byref(size)) == code, (rows, k)
+        assert lib.ddit_linear_mx4_workspace_bytes(rows, 64, k, C.byref(size)) == code
+    assert lib.ddit_mx4_bytes(1, 8, None, C.byref(size)) == -1 and lib.ddit_mx4_bytes(1, 8, C.byref(size), None) == -1
+    assert lib.ddit_linear_mx4_workspace_bytes(1, 0, 8, C.byref(size)) == -1 and lib.ddit_linear_mx4_workspace_bytes(1, 8, 8, None) == -1
+    q = _caller(lib.ddit_mx4_quantize, dict(x=P(0x1000), ld=64, rows=0, k=64, codes=P(0x2000), scales=P(0x3000), stream=None))
+    d = _caller(lib.ddit_mx4_dequantize, dict(codes=P(0x2000), scales=P(0x3000), rows=0, k=64, x=P(0x1000), ld=64, stream=None))
+    for call in (q, d):
+        assert call() == 0
+        for bad in (dict(x=None), dict(codes=None), dict(scales=None), dict(rows=-1), dict(k=0), dict(ld=56)):
+            assert call(**bad) == -1, bad
+        for bad in (dict(k=12), dict(rows=1 << 26)):
+            assert call(**bad) == -2, bad
+        for bad in (dict(ld=68), dict(x=P(0x1008)), dict(codes=P(0x2008)), dict(scales=P(0x3004))):
+            assert call(**bad) == -4, bad
+
+
+def test_linear_mx4_refusals(m):
+    lib = m.binding._lib
+    tail = dict(wc=P(0x3000), ws=P(0x4000), bias=None, N=0, n=64, k=64, out=P(0x5000), ld_out=64, resid=None, resid_out=None, table=None, c6=None,
+                gate_row=-1, tps=1)
+    dense = _caller(lib.ddit_linear_mx4_fwd, dict(epi=0, u=P(0x1000), ld_u=64, **tail, workspace=None, bytes=0, stream=None))
+    coded = _caller(lib.ddit_linear_mx4_codes_fwd, dict(epi=0, u=P(0x1000), us=P(0x2000), **tail, stream=None))
+    resid = dict(epi=2, resid=P(0x6000), resid_out=P(0x7000))
+    for call in (dense, coded):
+        assert call() == 0 and call(**resid) == 0 and call(**resid, out=None, ld_out=0) == 0
+        assert call(**resid, gate_row=5, table=P(0x8000), c6=P(0x9000)) == 0
+        for bad in (dict(epi=3), dict(epi=-1), dict(u=None), dict(wc=None), dict(ws=None), dict(N=-1), dict(n=0), dict(k=0), dict(out=None), dict(ld_out=56),
+                    dict(resid, resid=None), dict(resid, resid_out=None), dict(resid, gate_row=2), dict(resid, gate_row=6, table=P(0x8000), c6=P(0x9000)),
+                    dict(resid, gate_row=2, table=P(0x8000)), dict(resid, gate_row=2, table=P(0x8000), c6=P(0x9000), tps=0)):
+            assert call(**bad) == -1, bad
+        for bad in (dict(n=60), dict(k=60), dict(N=1 << 26), dict(n=1 << 26, ld_out=1 << 26)):
+            assert call(**bad) == -2, bad
+        for bad in (dict(ld_out=68), dict(u=P(0x1008)), dict(wc=P(0x3008)), dict(ws=P(0x4004)), dict(bias=P(0x8)), dict(out=P(0x5008)),
+                    dict(resid, resid=P(0x6008)), dict(resid, resid_out=P(0x7008)), dict(resid, gate_row=0, table=P(0x8004), c6=P(0x9000)),
+                    dict(resid, gate_row=0, table=P(0x8000), c6=P(0x9004))):
+            assert call(**bad) == -4, bad
+    assert coded(us=None) == -1 and coded(us=P(0x2008)) == -4
+    assert dense(ld_u=56) == -1 and dense(ld_u=68) == -4
+    need = m.ddit_linear_mx4_workspace_bytes(5, 64, 64)
+    assert dense(N=5) == -3 and dense(N=5, workspace=P(0x10000), bytes=need - 1) == -3 and str(need) in m.ddit_last_error()
+    assert dense(N=5, workspace=P(0x10010), bytes=need) == -4
