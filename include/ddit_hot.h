@@ -312,6 +312,24 @@ int ddit_linear_mx4_codes_fwd(int epilogue, const void *u_codes, const void *u_s
                               float *resid_out, const float *ada_table, const float *c6, int gate_row, int64_t tokens_per_sample,
                               void *hip_stream);
 
+/* Cross-attention of requests packed one behind the other, each to its own encoder states (another length for each, as
+ * the prompts of section 2.2's text condition have): for every b and head h, the queries in rows q_offsets[b] .. q_offsets[b+1]-1 of q attend
+ * to rows kv_offsets[b] .. kv_offsets[b+1]-1 of k and v,
+ *   o = softmax(scale q k^T) v,  lse = log(sum exp(scale q k^T)).
+ * q_offsets, kv_offsets: DEVICE int32 [B+1], not decreasing, within [0, q_rows] and [0, kv_rows]; they are read when the work
+ * runs, so a captured call serves other lengths of the same totals.  (Values outside are cut off at the arrays' ends; nothing outside is
+ * touched.)  A sequence may have no query, no state, or none that is left by key_mask_or_null: device uint8 [kv_rows], 0 = the state takes no
+ * part, whatever its values; such queries get o = 0 and lse = -inf.  Rows of o and lse that belong to no sequence stay as they are.
+ * q, o bf16 [q_rows, H, dh], k, v bf16 [kv_rows, H_kv, dh], rows ld_* elements apart (slices of wider buffers as in ddit_attn_fwd);
+ * query head h reads key head h / (H / H_kv).  dh: a multiple of 8, at most 128.  scale > 0.  lse_or_null fp32 [q_rows, H].
+ * o may not overlap an input.  workspace: ddit_cross_attn_packed_workspace_bytes() bytes, 256-byte aligned (NULL if 0), free again when the
+ * call's work is done; the bytes depend on the totals alone.  q_rows = 0: arguments are validated, nothing is enqueued. */
+int ddit_cross_attn_packed_workspace_bytes(int32_t B, int64_t q_rows, int64_t kv_rows, int32_t H, int32_t dh, size_t *bytes_out);
+int ddit_cross_attn_packed_fwd(const void *q, int64_t ld_q, const int32_t *q_offsets, const void *k, const void *v, int64_t ld_kv,
+                               const int32_t *kv_offsets, const uint8_t *key_mask_or_null, int32_t B, int64_t q_rows, int64_t kv_rows,
+                               int32_t H, int32_t H_kv, int32_t dh, float scale, void *o, int64_t ld_o, float *lse_or_null,
+                               void *workspace, size_t workspace_bytes, void *hip_stream);
+
 /* ---- output tiles of the linear: for tuning and for parity tests of every compiled tile ----
  * The linear is compiled for a short list of output tiles (rows x cols of out per workgroup), which callers can force, and for
  * a few forms beside the list.  ddit_linear_fwd takes, per call, a form for few tokens where its grid finds room on the device

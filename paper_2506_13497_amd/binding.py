@@ -35,7 +35,7 @@ EXPORTS = ["ddit_abi_version", "ddit_status_string", "ddit_last_error", "ddit_wo
            "ddit_buddy_create", "ddit_buddy_alloc", "ddit_buddy_release", "ddit_buddy_free_gpus", "ddit_buddy_destroy",
            "ddit_sched_simulate", "ddit_probe_mfma_bf16", "ddit_probe_stream_copy", "ddit_probe_stream_read", "ddit_probe_residual_stream",
            "ddit_branch_norms_fwd", "ddit_mx4_bytes", "ddit_mx4_quantize", "ddit_mx4_dequantize", "ddit_linear_mx4_workspace_bytes",
-           "ddit_linear_mx4_fwd", "ddit_linear_mx4_codes_fwd"]
+           "ddit_linear_mx4_fwd", "ddit_linear_mx4_codes_fwd", "ddit_cross_attn_packed_workspace_bytes", "ddit_cross_attn_packed_fwd"]
 
 
 class ddit_shape(C.Structure):
@@ -185,6 +185,8 @@ def _load() -> C.CDLL:
     lib.ddit_linear_mx4_workspace_bytes.argtypes = [I64, I32, I32, C.POINTER(SZ)]
     lib.ddit_linear_mx4_fwd.argtypes = [C.c_int, VP, I64, VP, VP, VP, I64, I32, I32, VP, I64, VP, VP, VP, VP, C.c_int, I64, VP, SZ, VP]
     lib.ddit_linear_mx4_codes_fwd.argtypes = [C.c_int, VP, VP, VP, VP, VP, I64, I32, I32, VP, I64, VP, VP, VP, VP, C.c_int, I64, VP]
+    lib.ddit_cross_attn_packed_workspace_bytes.argtypes = [I32, I64, I64, I32, I32, C.POINTER(SZ)]
+    lib.ddit_cross_attn_packed_fwd.argtypes = [VP, I64, VP, VP, VP, I64, VP, VP, I32, I64, I64, I32, I32, I32, C.c_float, VP, I64, VP, VP, SZ, VP]
     for n in EXPORTS:
         if n not in ("ddit_abi_version", "ddit_status_string", "ddit_last_error", "ddit_linear_tile_count"):
             getattr(lib, n).restype = C.c_int
@@ -576,6 +578,18 @@ def ddit_linear_mx4_codes_fwd(epilogue: int, u_codes, u_scales, W_codes, W_scale
                               resid_out=None, ada_table=None, c6=None, gate_row: int = -1, tokens_per_sample: int = 1) -> None:
     _check(_lib.ddit_linear_mx4_codes_fwd(epilogue, _ptr(u_codes), _ptr(u_scales), _ptr(W_codes), _ptr(W_scales), _ptr(bias), N, n, k, _ptr(out),
                                           ld_out, _ptr(resid), _ptr(resid_out), _ptr(ada_table), _ptr(c6), gate_row, tokens_per_sample, _stream()))
+
+
+def ddit_cross_attn_packed_workspace_bytes(B: int, q_rows: int, kv_rows: int, H: int, dh: int) -> int:
+    b = C.c_size_t(0)
+    _check(_lib.ddit_cross_attn_packed_workspace_bytes(B, q_rows, kv_rows, H, dh, C.byref(b)))
+    return int(b.value)
+
+
+def ddit_cross_attn_packed_fwd(q, ld_q: int, q_offsets, k, v, ld_kv: int, kv_offsets, key_mask, B: int, q_rows: int, kv_rows: int, H: int,
+                               H_kv: int, dh: int, scale: float, o, ld_o: int, lse=None, workspace=None) -> None:
+    _check(_lib.ddit_cross_attn_packed_fwd(_ptr(q), ld_q, _ptr(q_offsets), _ptr(k), _ptr(v), ld_kv, _ptr(kv_offsets), _ptr(key_mask), B, q_rows,
+                                           kv_rows, H, H_kv, dh, scale, _ptr(o), ld_o, _ptr(lse), _ptr(workspace), _nbytes(workspace), _stream()))
 
 
 def ddit_probe_mfma_bf16(operands, sink, iters: int) -> float:

@@ -11,7 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libddit_hot.so")
 SOURCES = ["ddit_hot.hip", "adaln_ln.hip", "gemm_bf16.hip", "flash_attn.hip", "temporal_attn.hip", "cond.hip",
            "latent_io.hip", "qk_norm_rope.hip", "step_scheduler.hip", "probes.hip",
-           "branch_norms.hip", "mx4.hip"]
+           "branch_norms.hip", "mx4.hip", "cross_attn.hip"]
 # packed-fp32 VALU forms are switched off for all device code of this library
 FLAGS = ["-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-Wall", "-Wno-unused-function",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]

@@ -217,6 +217,18 @@ struct Mx4GemmArgs {
 };
 int launch_mx4_gemm(int epilogue, const Mx4GemmArgs &a, hipStream_t s);
 
+// cross-attention of packed requests (cross_attn.hip)
+struct CrossAttnArgs {
+  const void *q, *k, *v; int64_t ld_q, ld_kv;
+  const int *q_off, *kv_off; const uint8_t *mask;   // device; mask may be null
+  int B; int64_t q_rows, kv_rows; int H, H_kv, dh;
+  float scale;
+  void *o; int64_t ld_o; float *lse;
+  float *scratch;                                   // cross_attn_parts() > 1: parts * q_rows * H * (dh + 2) floats
+};
+int cross_attn_parts(int B, int64_t q_rows, int64_t kv_rows, int H);   // in how many parts the keys are taken
+int launch_cross_attn(const CrossAttnArgs &a, hipStream_t s);
+
 // layers around the token-space step, solver
 int launch_position_code(float *pos, int Hp, int Wp, int D, hipStream_t s);
 int launch_patch_embed(const float *z, const void *W, const void *bias, const float *pos, void *x, int B, int Bz, int C,

@@ -1007,6 +1007,57 @@ int ddit_linear_mx4_fwd(int epilogue, const void *u, int64_t ld_u, const void *W
   return launch_mx4_gemm(epilogue, g, s);
 }
 
+static int check_cross_packed(int32_t B, int64_t q_rows, int64_t kv_rows, int32_t H, int32_t dh) {
+  if (B < 1 || q_rows < 0 || kv_rows < 0 || H < 1 || dh < 1) {
+    set_error("packed cross-attention: B=%d q_rows=%lld kv_rows=%lld H=%d dh=%d", B, (long long)q_rows, (long long)kv_rows, H, dh);
+    return DDIT_ERR_INVALID_ARG;
+  }
+  if (dh % 8 || dh > 128) { set_error("dh=%d: supported head dims are multiples of 8 up to 128", dh); return DDIT_ERR_UNSUPPORTED; }
+  if (B > 65536 || H > 65535 || q_rows > (int64_t)1 << 30 || kv_rows > (int64_t)1 << 30) {
+    set_error("packed cross-attention: B=%d H=%d q_rows=%lld kv_rows=%lld: too many", B, H, (long long)q_rows, (long long)kv_rows);
+    return DDIT_ERR_UNSUPPORTED;
+  }
+  return DDIT_OK;
+}
+
+int ddit_cross_attn_packed_workspace_bytes(int32_t B, int64_t q_rows, int64_t kv_rows, int32_t H, int32_t dh, size_t *bytes_out) {
+  DDIT_TRY(check_cross_packed(B, q_rows, kv_rows, H, dh));
+  if (!bytes_out) { set_error("bytes_out is NULL"); return DDIT_ERR_INVALID_ARG; }
+  const int parts = cross_attn_parts(B, q_rows, kv_rows, H);
+  *bytes_out = parts > 1 ? (size_t)parts * q_rows * H * (dh + 2) * 4 : 0;
+  return DDIT_OK;
+}
+
+int ddit_cross_attn_packed_fwd(const void *q, int64_t ld_q, const int32_t *q_offsets, const void *k, const void *v, int64_t ld_kv,
+                               const int32_t *kv_offsets, const uint8_t *key_mask_or_null, int32_t B, int64_t q_rows, int64_t kv_rows, int32_t H,
+                               int32_t H_kv, int32_t dh, float scale, void *o, int64_t ld_o, float *lse_or_null, void *workspace,
+                               size_t workspace_bytes, void *hip_stream) {
+  DDIT_TRY(check_cross_packed(B, q_rows, kv_rows, H, dh));
+  if (!q || !k || !v || !o || !q_offsets || !kv_offsets) { set_error("q, k, v, o, q_offsets and kv_offsets must not be NULL"); return DDIT_ERR_INVALID_ARG; }
+  if (H_kv < 1 || H % H_kv) { set_error("H=%d query heads do not share H_kv=%d key heads evenly", H, H_kv); return DDIT_ERR_INVALID_ARG; }
+  if (!(scale > 0.f) || !(scale - scale == 0.f)) { set_error("scale=%g must be positive and finite", (double)scale); return DDIT_ERR_INVALID_ARG; }
+  if (ld_q < (int64_t)H * dh || ld_kv < (int64_t)H_kv * dh || ld_o < (int64_t)H * dh) {
+    set_error("leading dimensions (%lld,%lld,%lld) must be at least H*dh=%lld, H_kv*dh=%lld, H*dh", (long long)ld_q, (long long)ld_kv, (long long)ld_o,
+              (long long)H * dh, (long long)H_kv * dh);
+    return DDIT_ERR_INVALID_ARG;
+  }
+  if (ld_q % 8 || ld_kv % 8 || ld_o % 8) { set_error("leading dimensions must be multiples of 8"); return DDIT_ERR_ALIGNMENT; }
+  for (const void *a : {q, k, v, (const void *)o})
+    if (!aligned16(a)) { set_error("q, k, v and o must be 16-byte aligned"); return DDIT_ERR_ALIGNMENT; }
+  for (const void *a : {(const void *)q_offsets, (const void *)kv_offsets, (const void *)lse_or_null})
+    if (reinterpret_cast<uintptr_t>(a) & 3u) { set_error("offsets and lse must be 4-byte aligned"); return DDIT_ERR_ALIGNMENT; }
+  if (q_rows == 0) return DDIT_OK;
+  size_t need = 0;
+  DDIT_TRY(ddit_cross_attn_packed_workspace_bytes(B, q_rows, kv_rows, H, dh, &need));
+  if (need) DDIT_TRY(check_ws(workspace, workspace_bytes, need));
+  CrossAttnArgs a;
+  memset(&a, 0, sizeof(a));
+  a.q = q; a.k = k; a.v = v; a.ld_q = ld_q; a.ld_kv = ld_kv; a.q_off = q_offsets; a.kv_off = kv_offsets; a.mask = key_mask_or_null;
+  a.B = B; a.q_rows = q_rows; a.kv_rows = kv_rows; a.H = H; a.H_kv = H_kv; a.dh = dh; a.scale = scale;
+  a.o = o; a.ld_o = ld_o; a.lse = lse_or_null; a.scratch = reinterpret_cast<float *>(workspace);
+  return launch_cross_attn(a, reinterpret_cast<hipStream_t>(hip_stream));
+}
+
 int ddit_linear_tile_count(void) { return gemm_tile_count(); }
 
 int ddit_linear_tile_info(int tile, int32_t *rows, int32_t *cols, int32_t *wavefronts, int32_t *workgroups_per_cu) {

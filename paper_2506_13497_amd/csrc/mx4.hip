@@ -127,7 +127,7 @@ __device__ __forceinline__ void wait_vmcnt() {
 #if defined(__HIP_DEVICE_COMPILE__)
 #define MX4_LOAD_TO_LDS(...) __builtin_amdgcn_raw_ptr_buffer_load_lds(__VA_ARGS__)
 #else
-#define MX4_LOAD_TO_LDS(r, ...) ((void)(r))
+#define MX4_LOAD_TO_LDS(r, at, size, lane_offset, offset, ...) ((void)(r), (void)(at), (void)(lane_offset), (void)(offset))
 #endif
 
 // v_mfma_scale_f32_32x32x64_f8f6f4 on 4-bit operands: lane l holds 32 consecutive k, one scaled block, of row l % 32: k half l / 32.

@@ -93,3 +93,30 @@ def test_linear_mx4_refusals(m):
     need = m.ddit_linear_mx4_workspace_bytes(5, 64, 64)
     assert dense(N=5) == -3 and dense(N=5, workspace=P(0x10000), bytes=need - 1) == -3 and str(need) in m.ddit_last_error()
     assert dense(N=5, workspace=P(0x10010), bytes=need) == -4
+
+
+def test_cross_packed_refusals(m):
+    lib = m.binding._lib
+    call = _caller(lib.ddit_cross_attn_packed_fwd, dict(
+        q=P(0x1000), ld_q=256, q_off=P(0x2000), k=P(0x3000), v=P(0x4000), ld_kv=128, kv_off=P(0x5000), mask=None, B=2, q_rows=0, kv_rows=10, H=4, G=2, dh=64,
+        scale=0.125, o=P(0x6000), ld_o=256, lse=None, ws=None, bytes=0, stream=None))
+    assert call() == 0 and call(mask=P(0x7001), lse=P(0x8004)) == 0
+    for bad in (dict(q=None), dict(k=None), dict(v=None), dict(o=None), dict(q_off=None), dict(kv_off=None), dict(B=0), dict(q_rows=-1), dict(kv_rows=-1), dict(H=0),
+                dict(G=0), dict(G=3), dict(dh=0), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")), dict(ld_q=248),
+                dict(ld_kv=120), dict(ld_o=248)):
+        assert call(**bad) == -1, bad
+    for bad in (dict(dh=60), dict(dh=136, ld_q=1024, ld_kv=1024, ld_o=1024), dict(B=1 << 20), dict(q_rows=1 << 31), dict(kv_rows=1 << 31), dict(H=1 << 17)):
+        assert call(**bad) == -2, bad
+    for bad in (dict(ld_q=260), dict(ld_kv=132), dict(ld_o=260), dict(q=P(0x1008)), dict(k=P(0x3008)), dict(v=P(0x4002)), dict(o=P(0x6008)), dict(q_off=P(0x2002)),
+                dict(kv_off=P(0x5001)), dict(lse=P(0x8002))):
+        assert call(**bad) == -4, bad
+    # a few queries against long encodings: parts of the keys, whose sums need room
+    few = dict(q_rows=10, kv_rows=8000)
+    need = m.ddit_cross_attn_packed_workspace_bytes(2, 10, 8000, 4, 64)
+    assert need > 0 and m.ddit_cross_attn_packed_workspace_bytes(2, 100000, 8000, 4, 64) == 0 and m.ddit_cross_attn_packed_workspace_bytes(2, 0, 8000, 4, 64) == 0
+    assert call(**few) == -3 and call(**few, ws=P(0x10000), bytes=need - 1) == -3 and str(need) in m.ddit_last_error()
+    assert call(**few, ws=P(0x10010), bytes=need) == -4
+    size = C.c_size_t()
+    assert lib.ddit_cross_attn_packed_workspace_bytes(0, 1, 1, 1, 64, C.byref(size)) == -1
+    assert lib.ddit_cross_attn_packed_workspace_bytes(1, 1, 1, 1, 60, C.byref(size)) == -2
+    assert lib.ddit_cross_attn_packed_workspace_bytes(1, 1, 1, 1, 64, None) == -1
