@@ -226,7 +226,7 @@ struct CrossAttnArgs {
   void *o; int64_t ld_o; float *lse;
   float *scratch;                                   // cross_attn_parts() > 1: parts * q_rows * H * (dh + 2) floats
 };
-int cross_attn_parts(int B, int64_t q_rows, int64_t kv_rows, int H);   // in how many parts the keys are taken
+int cross_attn_parts(int B, int64_t q_rows, int64_t kv_rows, int H, int H_kv);   // in how many parts the keys are taken
 int launch_cross_attn(const CrossAttnArgs &a, hipStream_t s);
 
 // layers around the token-space step, solver

@@ -1013,7 +1013,7 @@ static int check_cross_packed(int32_t B, int64_t q_rows, int64_t kv_rows, int32_
     return DDIT_ERR_INVALID_ARG;
   }
   if (dh % 8 || dh > 128) { set_error("dh=%d: supported head dims are multiples of 8 up to 128", dh); return DDIT_ERR_UNSUPPORTED; }
-  if (B > 65536 || H > 65535 || q_rows > (int64_t)1 << 30 || kv_rows > (int64_t)1 << 30) {
+  if (B > 65536 || H > 65535 || q_rows > ((int64_t)1 << 30) / H || kv_rows > (int64_t)1 << 30) {
     set_error("packed cross-attention: B=%d H=%d q_rows=%lld kv_rows=%lld: too many", B, H, (long long)q_rows, (long long)kv_rows);
     return DDIT_ERR_UNSUPPORTED;
   }
@@ -1023,7 +1023,9 @@ static int check_cross_packed(int32_t B, int64_t q_rows, int64_t kv_rows, int32_
 int ddit_cross_attn_packed_workspace_bytes(int32_t B, int64_t q_rows, int64_t kv_rows, int32_t H, int32_t dh, size_t *bytes_out) {
   DDIT_TRY(check_cross_packed(B, q_rows, kv_rows, H, dh));
   if (!bytes_out) { set_error("bytes_out is NULL"); return DDIT_ERR_INVALID_ARG; }
-  const int parts = cross_attn_parts(B, q_rows, kv_rows, H);
+  int parts = 1;   // the most that any number of key heads takes
+  for (int g = 1; g * g <= H; ++g)
+    if (H % g == 0) parts = std::max({parts, cross_attn_parts(B, q_rows, kv_rows, H, g), cross_attn_parts(B, q_rows, kv_rows, H, H / g)});
   *bytes_out = parts > 1 ? (size_t)parts * q_rows * H * (dh + 2) * 4 : 0;
   return DDIT_OK;
 }
