@@ -264,7 +264,8 @@ int ddit_self_attn_fwd(ddit_attn_kind kind, const ddit_shape *shape, void *q, vo
                        int64_t ld_kv, const void *g_q, const void *g_k, float *rope_table_or_null, int fuse, void *o,
                        int64_t ld_o, float *lse_or_null, void *hip_stream);
 
-/* ---- operators of models that differ from the step's layers: norms behind a branch, linears in four bits, packed requests ---- */
+/* ---- operators of models that differ from the step's layers: norms behind a branch, linears in four bits, packed requests ----
+ * A pointer to an array without elements (no token, no row, no encoder state) may be NULL. */
 
 typedef enum { DDIT_NORM_LAYER = 0, DDIT_NORM_RMS = 1 } ddit_norm_kind;
 
@@ -301,7 +302,7 @@ int ddit_mx4_dequantize(const void *codes, const void *scales, int64_t rows, int
  * ddit_mx4_quantize lays it out; bias bf16 [n] or NULL.  ddit_linear_mx4_fwd takes u bf16 [N,k] and quantises it on the way, in
  * a workspace (256-byte aligned, ddit_linear_mx4_workspace_bytes(); free again when the call's work is done);
  * ddit_linear_mx4_codes_fwd takes it quantised already, as by several linears that share u.  No output may overlap an input but
- * resid_out resid.  N = 0 as above. */
+ * resid_out resid.  n below 2^24, ld_out below 2^25.  N = 0 as above. */
 int ddit_linear_mx4_workspace_bytes(int64_t N, int32_t n, int32_t k, size_t *bytes_out);
 int ddit_linear_mx4_fwd(int epilogue, const void *u, int64_t ld_u, const void *W_codes, const void *W_scales, const void *bias, int64_t N,
                         int32_t n, int32_t k, void *out, int64_t ld_out, const float *resid, float *resid_out, const float *ada_table,

@@ -305,38 +305,37 @@ __global__ __launch_bounds__(64 * NW) void k_cross_attn(CrossParams p) {
   }
 }
 
-// The parts' sums of 32 rows of a key head meet: eight threads a row.  Each part's maximum is its reference; a part without weight is
-// left out.
+// The parts' sums of 4 rows of a key head meet, a wavefront a row: a lane looks after one part's maximum and sum first, then after two
+// features.  A part without weight is left out (its place in part_o may hold anything).
 __global__ __launch_bounds__(256) void k_cross_join(CrossParams p) {
   Slot slot;
-  if (!find_slot(p, blockIdx.x, 32, slot)) return;
-  const int r = slot.begin + (threadIdx.x >> 3), sub = threadIdx.x & 7, q = r / p.group;
+  if (!find_slot(p, blockIdx.x, 4, slot)) return;
+  const int lane = threadIdx.x & 63, r = slot.begin + (threadIdx.x >> 6), q = r / p.group;
   if (r >= slot.end) return;
   const int h = blockIdx.y * p.group + r - q * p.group;
   const int64_t token = slot.q_first + q, step = (int64_t)p.q_rows * p.H, at = token * p.H + h;
-  const float2 *const ml = reinterpret_cast<const float2 *>(p.part_ml) + at;
-  float top = -INFINITY;
-  for (int z = 0; z < p.parts; ++z) top = fmaxf(top, ml[z * step].x);
-  if (top == -INFINITY) top = 0.f;
-  float l = 0.f;
-  for (int z = 0; z < p.parts; ++z) l += ml[z * step].y * __builtin_amdgcn_exp2f((ml[z * step].x - top) * p.scale_log2);
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  for (int c = sub * 8; c < p.dh; c += 64) {
-    floatx4 a = {0.f, 0.f, 0.f, 0.f}, a1 = a;
-    for (int z = 0; z < p.parts; ++z) {
-      const float2 part = ml[z * step];
-      if (part.y == 0.f) continue;
-      const float w = __builtin_amdgcn_exp2f((part.x - top) * p.scale_log2);
-      const floatx4 *src = reinterpret_cast<const floatx4 *>(p.part_o + (at + z * step) * p.dh + c);
-      a += src[0] * w;
-      a1 += src[1] * w;
-    }
-    bf16x8 v;
+  float2 ml = make_float2(-INFINITY, 0.f);
+  if (lane < p.parts) ml = reinterpret_cast<const float2 *>(p.part_ml)[at + lane * step];
+  float top = ml.x;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) { v[e] = (bf16_t)(a[e] * inv); v[e + 4] = (bf16_t)(a1[e] * inv); }
-    *reinterpret_cast<bf16x8 *>(p.o + token * p.ld_o + h * p.dh + c) = v;
+  for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
+  const float weight = ml.y == 0.f ? 0.f : __builtin_amdgcn_exp2f((ml.x - top) * p.scale_log2);
+  const float l = wave_sum(ml.y * weight), inv = l == 0.f ? 0.f : 1.f / l;
+  const int c = std::min(2 * lane, p.dh - 2);
+  float2 a = make_float2(0.f, 0.f);
+
+  for (int z = 0; z < p.parts; ++z) {
+    const float w = __uint_as_float((unsigned)__builtin_amdgcn_readlane((int)__float_as_uint(weight), z));
+    const float2 v = *reinterpret_cast<const float2 *>(p.part_o + (at + z * step) * p.dh + c);
+    a.x += w == 0.f ? 0.f : v.x * w;
+    a.y += w == 0.f ? 0.f : v.y * w;
   }
-  if (p.lse && sub == 0) p.lse[at] = l == 0.f ? -INFINITY : __builtin_fmaf(top, p.scale, __builtin_amdgcn_logf(l) * 0.6931471805599453f);
+  if (2 * lane < p.dh) {
+    bf16x2 v;
+    v[0] = (bf16_t)(a.x * inv); v[1] = (bf16_t)(a.y * inv);
+    *reinterpret_cast<bf16x2 *>(p.o + token * p.ld_o + h * p.dh + c) = v;
+  }
+  if (p.lse && lane == 0) p.lse[at] = l == 0.f ? -INFINITY : __builtin_fmaf(top, p.scale, __builtin_amdgcn_logf(l) * 0.6931471805599453f);
 }
 
 template <int KS, int NW, int ST>
@@ -390,7 +389,7 @@ int launch_cross_attn(const CrossAttnArgs &a, hipStream_t s) {
   const int rc = p.dh <= 64 ? launch_form<4>(waves, p, s) : p.dh <= 80 ? launch_form<5>(waves, p, s) : p.dh <= 96 ? launch_form<6>(waves, p, s)
                                                                                                               : launch_form<8>(waves, p, s);
   if (rc != 0 || p.parts == 1) return rc;
-  hipLaunchKernelGGL(k_cross_join, dim3((unsigned)(rows / 32 + p.B), (unsigned)a.H_kv), dim3(256), 0, s, p);
+  hipLaunchKernelGGL(k_cross_join, dim3((unsigned)(rows / 4 + p.B), (unsigned)a.H_kv), dim3(256), 0, s, p);
   return hip_fail(hipGetLastError(), "packed cross-attention join");
 }
 

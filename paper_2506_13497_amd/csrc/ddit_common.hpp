@@ -206,7 +206,8 @@ inline int64_t mx4_panels(int64_t k) { return (k + 127) / 128; }
 int launch_mx4_quantize(const void *x, int64_t ld_x, int64_t rows, int k, void *codes, void *scales, hipStream_t s);
 int launch_mx4_dequantize(const void *codes, const void *scales, int64_t rows, int k, void *out, int64_t ld_out, hipStream_t s);
 struct Mx4GemmArgs {
-  const void *u_codes, *u_scales;     // [N, k] quantised
+  const void *u_codes, *u_scales;     // [N, k] quantised, or, where the launch quantises by itself (mx4_one_launch),
+  const void *u; int64_t ld_u;        // bf16; else null
   const void *w_codes, *w_scales;     // [n, k] quantised
   const void *bias;                   // bf16 [n] or null
   int64_t N; int n; int k;
@@ -215,6 +216,7 @@ struct Mx4GemmArgs {
   const float *gate_tab, *gate_c6; int64_t gate_c6_stride;   // as in GemmArgs
   int64_t tokens_per_sample;
 };
+bool mx4_one_launch(int64_t N, int n);   // whether a linear of N tokens and n features takes u as it is
 int launch_mx4_gemm(int epilogue, const Mx4GemmArgs &a, hipStream_t s);
 
 // cross-attention of packed requests (cross_attn.hip)

@@ -871,7 +871,7 @@ int ddit_branch_norms_fwd(int norm, const void *f, int64_t ld_f, const void *g_p
                           const float *next_table, int which, int64_t N, int64_t tokens_per_sample, int32_t D, float eps, void *out_or_null,
                           int64_t ld_out, void *hip_stream) {
   if (norm != DDIT_NORM_LAYER && norm != DDIT_NORM_RMS) { set_error("unknown norm %d", norm); return DDIT_ERR_INVALID_ARG; }
-  if (!f || !x || !x_out) { set_error("f, x and x_out must not be NULL"); return DDIT_ERR_INVALID_ARG; }
+  if (N > 0 && (!f || !x || !x_out)) { set_error("f, x and x_out must not be NULL"); return DDIT_ERR_INVALID_ARG; }
   if (N < 0 || tokens_per_sample < 1 || D < 1 || !(eps > 0.f) || gate_row > 5 || which > 1) {
     set_error("branch_norms: N=%lld tokens_per_sample=%lld D=%d eps=%g gate_row=%d which=%d", (long long)N, (long long)tokens_per_sample, D,
               (double)eps, gate_row, which);
@@ -885,7 +885,7 @@ int ddit_branch_norms_fwd(int norm, const void *f, int64_t ld_f, const void *g_p
   if (ld_f % 8 || (out_or_null && ld_out % 8)) { set_error("leading dimensions must be multiples of 8"); return DDIT_ERR_ALIGNMENT; }
   if (gate_row >= 0 && (!gate_table || !c6)) { set_error("gate_row=%d needs gate_table and c6", gate_row); return DDIT_ERR_INVALID_ARG; }
   if (which >= 0 && (!next_table || !c6)) { set_error("which=%d needs next_table and c6", which); return DDIT_ERR_INVALID_ARG; }
-  if (which >= 0 && !out_or_null) { set_error("which=%d modulates an output that is not given", which); return DDIT_ERR_INVALID_ARG; }
+  if (N > 0 && which >= 0 && !out_or_null) { set_error("which=%d modulates an output that is not given", which); return DDIT_ERR_INVALID_ARG; }
   for (const void *q : {f, g_post_or_null, (const void *)x, (const void *)gate_table, (const void *)c6, (const void *)x_out, g_pre_or_null,
                         (const void *)next_table, (const void *)out_or_null})
     if (q && !aligned16(q)) { set_error("pointers must be 16-byte aligned"); return DDIT_ERR_ALIGNMENT; }
@@ -919,7 +919,7 @@ int ddit_mx4_bytes(int64_t rows, int32_t k, size_t *code_bytes_out, size_t *scal
 
 static int check_mx4_copy(const void *dense, int64_t ld, int64_t rows, int32_t k, const void *codes, const void *scales) {
   DDIT_TRY(check_mx4(rows, k, "rows"));
-  if (!dense || !codes || !scales) { set_error("the values, codes and scales must not be NULL"); return DDIT_ERR_INVALID_ARG; }
+  if (rows > 0 && (!dense || !codes || !scales)) { set_error("the values, codes and scales must not be NULL"); return DDIT_ERR_INVALID_ARG; }
   if (ld < k) { set_error("leading dimension %lld below k=%d", (long long)ld, k); return DDIT_ERR_INVALID_ARG; }
   if (ld % 8 || !aligned16(dense) || !aligned16(codes) || !aligned16(scales)) {
     set_error("pointers must be 16-byte aligned and leading dimensions multiples of 8"); return DDIT_ERR_ALIGNMENT;
@@ -955,9 +955,10 @@ static int check_linear_mx4(int epilogue, const void *W_codes, const void *W_sca
   DDIT_TRY(check_mx4(N, k, "N"));
   DDIT_TRY(check_mx4(n, k, "n"));
   if (n % 8) { set_error("n=%d must be a multiple of 8", n); return DDIT_ERR_UNSUPPORTED; }
+  if (n >= 1 << 24 || (out && ld_out >= 1 << 25)) { set_error("n=%d, ld_out=%lld: rows of the output are too long", n, (long long)ld_out); return DDIT_ERR_UNSUPPORTED; }
   memset(g, 0, sizeof(*g));
   if (epilogue == DDIT_EPI_RESIDUAL_F32) {
-    if (!resid || !resid_out) { set_error("resid and resid_out must not be NULL for the residual epilogue"); return DDIT_ERR_INVALID_ARG; }
+    if (N > 0 && (!resid || !resid_out)) { set_error("resid and resid_out must not be NULL for the residual epilogue"); return DDIT_ERR_INVALID_ARG; }
     if (gate_row >= 0) {
       if (gate_row > 5 || !ada_table || !c6) { set_error("gate_row=%d needs ada_table and c6, and must be < 6", gate_row); return DDIT_ERR_INVALID_ARG; }
       if (tokens_per_sample < 1) { set_error("tokens_per_sample=%lld", (long long)tokens_per_sample); return DDIT_ERR_INVALID_ARG; }
@@ -965,7 +966,7 @@ static int check_linear_mx4(int epilogue, const void *W_codes, const void *W_sca
       g->gate_c6 = c6 + (int64_t)gate_row * n;
       g->gate_c6_stride = 6 * (int64_t)n;
     }
-  } else if (!out) {
+  } else if (N > 0 && !out) {
     set_error("out must not be NULL"); return DDIT_ERR_INVALID_ARG;
   }
   if (out && ld_out < n) { set_error("ld_out=%lld below n=%d", (long long)ld_out, n); return DDIT_ERR_INVALID_ARG; }
@@ -981,7 +982,7 @@ int ddit_linear_mx4_codes_fwd(int epilogue, const void *u_codes, const void *u_s
                               int64_t N, int32_t n, int32_t k, void *out, int64_t ld_out, const float *resid, float *resid_out,
                               const float *ada_table, const float *c6, int gate_row, int64_t tokens_per_sample, void *hip_stream) {
   Mx4GemmArgs g;
-  if (!u_codes || !u_scales) { set_error("u_codes and u_scales must not be NULL"); return DDIT_ERR_INVALID_ARG; }
+  if (N > 0 && (!u_codes || !u_scales)) { set_error("u_codes and u_scales must not be NULL"); return DDIT_ERR_INVALID_ARG; }
   DDIT_TRY(check_linear_mx4(epilogue, W_codes, W_scales, bias, N, n, k, out, ld_out, resid, resid_out, ada_table, c6, gate_row, tokens_per_sample, &g));
   if (!aligned16(u_codes) || !aligned16(u_scales)) { set_error("pointers must be 16-byte aligned"); return DDIT_ERR_ALIGNMENT; }
   g.u_codes = u_codes; g.u_scales = u_scales;
@@ -992,7 +993,7 @@ int ddit_linear_mx4_fwd(int epilogue, const void *u, int64_t ld_u, const void *W
                         int32_t n, int32_t k, void *out, int64_t ld_out, const float *resid, float *resid_out, const float *ada_table,
                         const float *c6, int gate_row, int64_t tokens_per_sample, void *workspace, size_t workspace_bytes, void *hip_stream) {
   Mx4GemmArgs g;
-  if (!u) { set_error("u must not be NULL"); return DDIT_ERR_INVALID_ARG; }
+  if (N > 0 && !u) { set_error("u must not be NULL"); return DDIT_ERR_INVALID_ARG; }
   DDIT_TRY(check_linear_mx4(epilogue, W_codes, W_scales, bias, N, n, k, out, ld_out, resid, resid_out, ada_table, c6, gate_row, tokens_per_sample, &g));
   if (ld_u < k) { set_error("linear: ld_u=%lld below k=%d", (long long)ld_u, k); return DDIT_ERR_INVALID_ARG; }
   if (ld_u % 8 || !aligned16(u)) { set_error("u must be 16-byte aligned and ld_u a multiple of 8"); return DDIT_ERR_ALIGNMENT; }
@@ -1000,6 +1001,10 @@ int ddit_linear_mx4_fwd(int epilogue, const void *u, int64_t ld_u, const void *W
   size_t need = 0;
   DDIT_TRY(ddit_linear_mx4_workspace_bytes(N, n, k, &need));
   DDIT_TRY(check_ws(workspace, workspace_bytes, need));
+  if (mx4_one_launch(N, n)) {
+    g.u = u; g.ld_u = ld_u;
+    return launch_mx4_gemm(epilogue, g, reinterpret_cast<hipStream_t>(hip_stream));
+  }
   unsigned char *ws = reinterpret_cast<unsigned char *>(workspace);
   g.u_codes = ws; g.u_scales = ws + align_up((size_t)N * mx4_panels(k) * 64);
   hipStream_t s = reinterpret_cast<hipStream_t>(hip_stream);
@@ -1035,7 +1040,9 @@ int ddit_cross_attn_packed_fwd(const void *q, int64_t ld_q, const int32_t *q_off
                                int32_t H_kv, int32_t dh, float scale, void *o, int64_t ld_o, float *lse_or_null, void *workspace,
                                size_t workspace_bytes, void *hip_stream) {
   DDIT_TRY(check_cross_packed(B, q_rows, kv_rows, H, dh));
-  if (!q || !k || !v || !o || !q_offsets || !kv_offsets) { set_error("q, k, v, o, q_offsets and kv_offsets must not be NULL"); return DDIT_ERR_INVALID_ARG; }
+  if ((q_rows > 0 && (!q || !o)) || (kv_rows > 0 && (!k || !v)) || !q_offsets || !kv_offsets) {
+    set_error("q, k, v, o, q_offsets and kv_offsets must not be NULL"); return DDIT_ERR_INVALID_ARG;
+  }
   if (H_kv < 1 || H % H_kv) { set_error("H=%d query heads do not share H_kv=%d key heads evenly", H, H_kv); return DDIT_ERR_INVALID_ARG; }
   if (!(scale > 0.f) || !(scale - scale == 0.f)) { set_error("scale=%g must be positive and finite", (double)scale); return DDIT_ERR_INVALID_ARG; }
   if (ld_q < (int64_t)H * dh || ld_kv < (int64_t)H_kv * dh || ld_o < (int64_t)H * dh) {

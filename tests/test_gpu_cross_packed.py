@@ -242,3 +242,13 @@ def test_a_captured_call_serves_other_lengths(m, R, K):
         ro, eo, rl, el = reference(q, k, v, a, b, mask, H, G, dh, 0.1)
         own = ~rl[:, 0].isnan()
         assert ((o[own].double() - ro[own]).abs() <= eo[own]).all()
+
+
+def test_no_states_and_no_queries_at_all(m):
+    H, dh = 2, 64
+    q, kv, _ = inputs(9, 20, H, H, dh, 1)
+    o, lse = run(m, q, kv[:0, :H * dh], kv[:0, H * dh:], [0, 4, 9], [0, 0, 0], None, H, H, dh, 0.1, H * dh, 2 * H * dh, K=0)
+    assert (o == 0).all() and (lse == -math.inf).all()
+    off = torch.zeros(2, dtype=torch.int32, device="cuda")
+    m.ddit_cross_attn_packed_fwd(q[:0], H * dh, off, kv, kv, 2 * H * dh, off, None, 1, 0, 20, H, H, dh, 0.1, o[:0], H * dh, lse[:0], None)
+    torch.cuda.synchronize()

@@ -272,3 +272,21 @@ def test_captured_and_on_another_stream(m, N):
         call(other, ws2)
         torch.cuda.synchronize()
         assert _same_values(out, other)
+
+
+def test_tensors_of_another_device_and_empty_ones(m):
+    """A tensor on the host is refused, not read by the GPU; calls on nothing do nothing, though torch gives nothing no address."""
+    k, n = 64, 72
+    t = _problem(m, 4, n, k, 2)
+    out, ws = torch.empty((4, n), dtype=torch.bfloat16, device="cuda"), torch.empty(4096, dtype=torch.uint8, device="cuda")
+    for bad in (dict(u=t["u"].cpu()), dict(bias=t["bias"].cpu()), dict(out=out.cpu())):
+        a = dict(u=t["u"], bias=t["bias"], out=out, **{})
+        a.update(bad)
+        with pytest.raises(m.DditError) as e:
+            m.ddit_linear_mx4_fwd(0, a["u"], k, t["wc"], t["ws"], a["bias"], 4, n, k, a["out"], n, ws)
+        assert e.value.status == m.DDIT_ERR_INVALID_ARG and "cpu" in str(e.value)
+    m.ddit_linear_mx4_fwd(0, t["u"][:0], k, t["wc"], t["ws"], None, 0, n, k, out[:0], n, ws[:0])
+    m.ddit_linear_mx4_codes_fwd(0, t["uc"][:, :0], t["us"][:, :0], t["wc"], t["ws"], None, 0, n, k, out[:0], n)
+    m.ddit_mx4_quantize(t["u"][:0], k, 0, k, t["uc"][:, :0], t["us"][:, :0])
+    m.ddit_branch_norms_fwd(0, out[:0], n, None, t["x"][:0], 1.0, t["table"], t["c6"](4), 2, t["x"][:0], None, t["table"], 1, 4, 1e-6, out[:0], n)
+    torch.cuda.synchronize()

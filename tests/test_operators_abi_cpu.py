@@ -30,9 +30,10 @@ def test_branch_norms_refusals(m):
     assert call() == 0 and call(x_out=P(0x2000)) == 0          # zero tokens: checked, and nothing done
     assert call(gate_row=-1, which=-1, gate_table=None, next_table=None, c6=None) == 0
     assert call(which=-1, out=None, ld_out=0) == 0
-    for bad in (dict(norm=2), dict(norm=-1), dict(f=None), dict(x=None), dict(x_out=None), dict(N=-1), dict(tps=0), dict(D=0), dict(eps=0.0),
+    assert call(f=None, x=None, x_out=None, out=None) == 0     # nothing has no address
+    for bad in (dict(norm=2), dict(norm=-1), dict(N=3, f=None), dict(N=3, x=None), dict(N=3, x_out=None), dict(N=-1), dict(tps=0), dict(D=0), dict(eps=0.0),
                 dict(eps=float("nan")), dict(gate_row=6), dict(which=2), dict(r=float("inf")), dict(r=float("nan")), dict(ld_f=56), dict(ld_out=56),
-                dict(gate_table=None), dict(c6=None), dict(next_table=None), dict(c6=None, which=-1), dict(out=None)):
+                dict(gate_table=None), dict(c6=None), dict(next_table=None), dict(c6=None, which=-1), dict(N=3, out=None)):
         assert call(**bad) == -1, bad
         assert m.ddit_last_error()
     for bad in (dict(D=60, ld_f=64), dict(D=8200, ld_f=8200, ld_out=8200), dict(N=1 << 50)):
@@ -59,8 +60,8 @@ def test_mx4_sizes_and_refusals(m):
     q = _caller(lib.ddit_mx4_quantize, dict(x=P(0x1000), ld=64, rows=0, k=64, codes=P(0x2000), scales=P(0x3000), stream=None))
     d = _caller(lib.ddit_mx4_dequantize, dict(codes=P(0x2000), scales=P(0x3000), rows=0, k=64, x=P(0x1000), ld=64, stream=None))
     for call in (q, d):
-        assert call() == 0
-        for bad in (dict(x=None), dict(codes=None), dict(scales=None), dict(rows=-1), dict(k=0), dict(ld=56)):
+        assert call() == 0 and call(x=None, codes=None, scales=None) == 0
+        for bad in (dict(rows=3, x=None), dict(rows=3, codes=None), dict(rows=3, scales=None), dict(rows=-1), dict(k=0), dict(ld=56)):
             assert call(**bad) == -1, bad
         for bad in (dict(k=12), dict(rows=1 << 26)):
             assert call(**bad) == -2, bad
@@ -78,17 +79,18 @@ def test_linear_mx4_refusals(m):
     for call in (dense, coded):
         assert call() == 0 and call(**resid) == 0 and call(**resid, out=None, ld_out=0) == 0
         assert call(**resid, gate_row=5, table=P(0x8000), c6=P(0x9000)) == 0
-        for bad in (dict(epi=3), dict(epi=-1), dict(u=None), dict(wc=None), dict(ws=None), dict(N=-1), dict(n=0), dict(k=0), dict(out=None), dict(ld_out=56),
-                    dict(resid, resid=None), dict(resid, resid_out=None), dict(resid, gate_row=2), dict(resid, gate_row=6, table=P(0x8000), c6=P(0x9000)),
+        assert call(u=None, out=None) == 0 and call(epi=2, u=None, out=None) == 0
+        for bad in (dict(epi=3), dict(epi=-1), dict(N=3, u=None), dict(wc=None), dict(ws=None), dict(N=-1), dict(n=0), dict(k=0), dict(N=3, out=None), dict(ld_out=56),
+                    dict(resid, N=3, resid=None), dict(resid, N=3, resid_out=None), dict(resid, gate_row=2), dict(resid, gate_row=6, table=P(0x8000), c6=P(0x9000)),
                     dict(resid, gate_row=2, table=P(0x8000)), dict(resid, gate_row=2, table=P(0x8000), c6=P(0x9000), tps=0)):
             assert call(**bad) == -1, bad
-        for bad in (dict(n=60), dict(k=60), dict(N=1 << 26), dict(n=1 << 26, ld_out=1 << 26)):
+        for bad in (dict(n=60), dict(k=60), dict(N=1 << 26), dict(n=1 << 26, ld_out=1 << 26), dict(n=1 << 24, ld_out=1 << 24), dict(ld_out=1 << 25)):
             assert call(**bad) == -2, bad
         for bad in (dict(ld_out=68), dict(u=P(0x1008)), dict(wc=P(0x3008)), dict(ws=P(0x4004)), dict(bias=P(0x8)), dict(out=P(0x5008)),
                     dict(resid, resid=P(0x6008)), dict(resid, resid_out=P(0x7008)), dict(resid, gate_row=0, table=P(0x8004), c6=P(0x9000)),
                     dict(resid, gate_row=0, table=P(0x8000), c6=P(0x9004))):
             assert call(**bad) == -4, bad
-    assert coded(us=None) == -1 and coded(us=P(0x2008)) == -4
+    assert coded(N=3, us=None) == -1 and coded(us=P(0x2008)) == -4
     assert dense(ld_u=56) == -1 and dense(ld_u=68) == -4
     need = m.ddit_linear_mx4_workspace_bytes(5, 64, 64)
     assert dense(N=5) == -3 and dense(N=5, workspace=P(0x10000), bytes=need - 1) == -3 and str(need) in m.ddit_last_error()
@@ -101,7 +103,8 @@ def test_cross_packed_refusals(m):
         q=P(0x1000), ld_q=256, q_off=P(0x2000), k=P(0x3000), v=P(0x4000), ld_kv=128, kv_off=P(0x5000), mask=None, B=2, q_rows=0, kv_rows=10, H=4, G=2, dh=64,
         scale=0.125, o=P(0x6000), ld_o=256, lse=None, ws=None, bytes=0, stream=None))
     assert call() == 0 and call(mask=P(0x7001), lse=P(0x8004)) == 0
-    for bad in (dict(q=None), dict(k=None), dict(v=None), dict(o=None), dict(q_off=None), dict(kv_off=None), dict(B=0), dict(q_rows=-1), dict(kv_rows=-1), dict(H=0),
+    assert call(q=None, o=None) == 0 and call(kv_rows=0, k=None, v=None) == 0
+    for bad in (dict(q_rows=3, q=None), dict(k=None), dict(v=None), dict(q_rows=3, o=None), dict(q_off=None), dict(kv_off=None), dict(B=0), dict(q_rows=-1), dict(kv_rows=-1), dict(H=0),
                 dict(G=0), dict(G=3), dict(dh=0), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")), dict(ld_q=248),
                 dict(ld_kv=120), dict(ld_o=248)):
         assert call(**bad) == -1, bad
