@@ -205,8 +205,28 @@ def _ptr(t: Optional[torch.Tensor]):
     return None if t is None else C.c_void_p(t.data_ptr())
 
 
+# The current stream's handle without the Stream object around it, whose making takes as long as a kernel launch (2.8 us of 3.1).
+_raw_stream, _device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+
+
 def _stream():
-    return C.c_void_p(torch.cuda.current_stream().cuda_stream)
+    return C.c_void_p(_raw_stream(_device()))
+
+
+def _on_device(*tensors):
+    """Addresses of tensors (None: NULL), behind them the current stream.  A tensor that is not on the current device, the one whose
+    stream the work goes to, is refused: its address would mean nothing there."""
+    dev = _device()
+    out = []
+    for t in tensors:
+        if t is None:
+            out.append(None)
+        elif t.get_device() == dev:
+            out.append(t.data_ptr())
+        else:
+            raise DditError(DDIT_ERR_INVALID_ARG, "a tensor is on %s, the current device is cuda:%d" % (t.device, dev))
+    out.append(_raw_stream(dev))
+    return out
 
 
 def make_shape(B, T, Hp, Wp, D, H, dh, M, Ly, n_blocks, flags=0, ln_eps=1e-6) -> ddit_shape:
@@ -540,10 +560,10 @@ def ddit_sample(shape: ddit_shape, weights: ddit_step_weights, io: ddit_io_weigh
 
 def ddit_branch_norms_fwd(norm: int, f, ld_f: int, g_post, x, residual_scale: float, gate_table, c6, gate_row: int, x_out, g_pre, next_table,
                           which: int, tokens_per_sample: int, eps: float, out, ld_out: int) -> None:
-    N, D = x.shape[0], x.shape[1]
-    _check(_lib.ddit_branch_norms_fwd(norm, _ptr(f), ld_f, _ptr(g_post), _ptr(x), residual_scale, _ptr(gate_table), _ptr(c6), gate_row,
-                                      _ptr(x_out), _ptr(g_pre), _ptr(next_table), which, N, tokens_per_sample, D, eps, _ptr(out), ld_out,
-                                      _stream()))
+    N, D = x.shape
+    pf, gp, px, gt, pc, po, gn, nt, ph, stream = _on_device(f, g_post, x, gate_table, c6, x_out, g_pre, next_table, out)
+    _check(_lib.ddit_branch_norms_fwd(norm, pf, ld_f, gp, px, residual_scale, gt, pc, gate_row, po, gn, nt, which, N, tokens_per_sample, D, eps, ph,
+                                      ld_out, stream))
 
 
 def ddit_mx4_bytes(rows: int, k: int):
@@ -554,11 +574,13 @@ def ddit_mx4_bytes(rows: int, k: int):
 
 
 def ddit_mx4_quantize(x, ld_x: int, rows: int, k: int, codes, scales) -> None:
-    _check(_lib.ddit_mx4_quantize(_ptr(x), ld_x, rows, k, _ptr(codes), _ptr(scales), _stream()))
+    px, pc, ps, stream = _on_device(x, codes, scales)
+    _check(_lib.ddit_mx4_quantize(px, ld_x, rows, k, pc, ps, stream))
 
 
 def ddit_mx4_dequantize(codes, scales, rows: int, k: int, out, ld_out: int) -> None:
-    _check(_lib.ddit_mx4_dequantize(_ptr(codes), _ptr(scales), rows, k, _ptr(out), ld_out, _stream()))
+    pc, ps, po, stream = _on_device(codes, scales, out)
+    _check(_lib.ddit_mx4_dequantize(pc, ps, rows, k, po, ld_out, stream))
 
 
 def ddit_linear_mx4_workspace_bytes(N: int, n: int, k: int) -> int:
@@ -569,15 +591,15 @@ def ddit_linear_mx4_workspace_bytes(N: int, n: int, k: int) -> int:
 
 def ddit_linear_mx4_fwd(epilogue: int, u, ld_u: int, W_codes, W_scales, bias, N: int, n: int, k: int, out, ld_out: int, workspace, resid=None,
                         resid_out=None, ada_table=None, c6=None, gate_row: int = -1, tokens_per_sample: int = 1) -> None:
-    _check(_lib.ddit_linear_mx4_fwd(epilogue, _ptr(u), ld_u, _ptr(W_codes), _ptr(W_scales), _ptr(bias), N, n, k, _ptr(out), ld_out, _ptr(resid),
-                                    _ptr(resid_out), _ptr(ada_table), _ptr(c6), gate_row, tokens_per_sample, _ptr(workspace),
-                                    _nbytes(workspace), _stream()))
+    pu, wc, ws, pb, po, px, pxo, pt, pc, pw, stream = _on_device(u, W_codes, W_scales, bias, out, resid, resid_out, ada_table, c6, workspace)
+    _check(_lib.ddit_linear_mx4_fwd(epilogue, pu, ld_u, wc, ws, pb, N, n, k, po, ld_out, px, pxo, pt, pc, gate_row, tokens_per_sample, pw,
+                                    _nbytes(workspace), stream))
 
 
 def ddit_linear_mx4_codes_fwd(epilogue: int, u_codes, u_scales, W_codes, W_scales, bias, N: int, n: int, k: int, out, ld_out: int, resid=None,
                               resid_out=None, ada_table=None, c6=None, gate_row: int = -1, tokens_per_sample: int = 1) -> None:
-    _check(_lib.ddit_linear_mx4_codes_fwd(epilogue, _ptr(u_codes), _ptr(u_scales), _ptr(W_codes), _ptr(W_scales), _ptr(bias), N, n, k, _ptr(out),
-                                          ld_out, _ptr(resid), _ptr(resid_out), _ptr(ada_table), _ptr(c6), gate_row, tokens_per_sample, _stream()))
+    uc, us, wc, ws, pb, po, px, pxo, pt, pc, stream = _on_device(u_codes, u_scales, W_codes, W_scales, bias, out, resid, resid_out, ada_table, c6)
+    _check(_lib.ddit_linear_mx4_codes_fwd(epilogue, uc, us, wc, ws, pb, N, n, k, po, ld_out, px, pxo, pt, pc, gate_row, tokens_per_sample, stream))
 
 
 def ddit_cross_attn_packed_workspace_bytes(B: int, q_rows: int, kv_rows: int, H: int, dh: int) -> int:
@@ -588,8 +610,9 @@ def ddit_cross_attn_packed_workspace_bytes(B: int, q_rows: int, kv_rows: int, H:
 
 def ddit_cross_attn_packed_fwd(q, ld_q: int, q_offsets, k, v, ld_kv: int, kv_offsets, key_mask, B: int, q_rows: int, kv_rows: int, H: int,
                                H_kv: int, dh: int, scale: float, o, ld_o: int, lse=None, workspace=None) -> None:
-    _check(_lib.ddit_cross_attn_packed_fwd(_ptr(q), ld_q, _ptr(q_offsets), _ptr(k), _ptr(v), ld_kv, _ptr(kv_offsets), _ptr(key_mask), B, q_rows,
-                                           kv_rows, H, H_kv, dh, scale, _ptr(o), ld_o, _ptr(lse), _ptr(workspace), _nbytes(workspace), _stream()))
+    pq, qo, pk, pv, ko, pm, po, pl, pw, stream = _on_device(q, q_offsets, k, v, kv_offsets, key_mask, o, lse, workspace)
+    _check(_lib.ddit_cross_attn_packed_fwd(pq, ld_q, qo, pk, pv, ld_kv, ko, pm, B, q_rows, kv_rows, H, H_kv, dh, scale, po, ld_o, pl, pw,
+                                           _nbytes(workspace), stream))
 
 
 def ddit_probe_mfma_bf16(operands, sink, iters: int) -> float:
