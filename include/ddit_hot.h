@@ -324,7 +324,8 @@ int ddit_linear_mx4_codes_fwd(int epilogue, const void *u_codes, const void *u_s
  * q, o bf16 [q_rows, H, dh], k, v bf16 [kv_rows, H_kv, dh], rows ld_* elements apart (slices of wider buffers as in ddit_attn_fwd);
  * query head h reads key head h / (H / H_kv).  dh: a multiple of 8, at most 128.  scale > 0.  lse_or_null fp32 [q_rows, H].
  * o may not overlap an input.  workspace: ddit_cross_attn_packed_workspace_bytes() bytes, 256-byte aligned (NULL if 0), free again when the
- * call's work is done; the bytes depend on the totals alone.  q_rows * H up to 2^30.  q_rows = 0: arguments are validated, nothing is enqueued. */
+ * call's work is done; the bytes depend on the totals alone.  q_rows * H up to 2^30, leading
+ * dimensions below 2^22.  q_rows = 0: arguments are validated, nothing is enqueued. */
 int ddit_cross_attn_packed_workspace_bytes(int32_t B, int64_t q_rows, int64_t kv_rows, int32_t H, int32_t dh, size_t *bytes_out);
 int ddit_cross_attn_packed_fwd(const void *q, int64_t ld_q, const int32_t *q_offsets, const void *k, const void *v, int64_t ld_kv,
                                const int32_t *kv_offsets, const uint8_t *key_mask_or_null, int32_t B, int64_t q_rows, int64_t kv_rows,

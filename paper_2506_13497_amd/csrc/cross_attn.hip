@@ -19,6 +19,7 @@
 #include "ddit_common.hpp"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace {
 
@@ -29,6 +30,19 @@ typedef short shortx8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) shortx4 *lds_s4_ptr_t;
 
 constexpr int KT = 64;   // keys of a tile
+
+// Lanes l and l + 32 exchange: the upper lanes' a against the lower lanes' b.
+struct Swapped { unsigned a, b; };
+__device__ __forceinline__ Swapped swap_halves(unsigned a, unsigned b) {
+  const uintx2 r = __builtin_bit_cast(uintx2, __builtin_amdgcn_permlane32_swap(a, b, false, false));
+  return {r[0], r[1]};
+}
+
+// The same within the halves: lanes 16-31 and 48-63 of a against lanes 0-15 and 32-47 of b.
+__device__ __forceinline__ Swapped swap_quarters(unsigned a, unsigned b) {
+  const uintx2 r = __builtin_bit_cast(uintx2, __builtin_amdgcn_permlane16_swap(a, b, false, false));
+  return {r[0], r[1]};
+}
 
 struct CrossParams {
   const bf16_t *q, *k, *v;
@@ -97,42 +111,56 @@ __global__ __launch_bounds__(64 * NW) void k_cross_attn(CrossParams p) {
   constexpr int QT = 32 * NW, CJ = (KT * C::CH + 64 * NW - 1) / (64 * NW);   // pieces of a tile that a thread stages
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l32 = lane & 31, lh = lane >> 5;
+  // Workgroups are dealt out to the 8 XCDs in turn.  The heads of a slot come one after the other on one XCD: a row of one head is 2 dh bytes
+  // of the token's, so heads share the cache lines of q and o, which its L2 puts together.
+  const int H_kv = p.H / p.group, i0 = blockIdx.x >> 3, i1 = i0 / H_kv, kv_head = i0 - i1 * H_kv;
+  const int i2 = i1 / p.parts, part = i1 - i2 * p.parts;
   Slot slot;
-  if (!find_slot(p, blockIdx.x, p.run, slot)) return;
-  const int h0 = blockIdx.y * p.group;   // first of the key head's query heads
+  if (!find_slot(p, (unsigned)i2 * 8 + (blockIdx.x & 7), p.run, slot)) return;
+  const int h0 = kv_head * p.group;   // first of the key head's query heads
   const int n_keys = slot.kv_end - slot.kv_begin, all = (n_keys + KT - 1) / KT;
-  const int t_begin = (int)((int64_t)all * blockIdx.z / p.parts), t_end = (int)((int64_t)all * (blockIdx.z + 1) / p.parts);
+  const int t_begin = (int)((int64_t)all * part / p.parts), t_end = (int)((int64_t)all * (part + 1) / p.parts);
   const int n_tiles = t_end - t_begin, pieces = p.dh >> 3;
 
-  bf16x8 qn[KS];   // the next row tile's fragments
-  auto fetch_q = [&](int r0) {
-    const int r = std::min(r0 + wave * 32 + l32, slot.end - 1), q = r / p.group;
-    const bf16_t *row = p.q + (int64_t)(slot.q_first + q) * p.ld_q + (h0 + r - q * p.group) * p.dh;
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) qn[ks][e] = (bf16_t)0.f;
-      if (2 * ks + lh < pieces) qn[ks] = *reinterpret_cast<const bf16x8 *>(row + 16 * ks + 8 * lh);
-    }
+  // Everything is loaded through buffers: what lies past an end, or is sent there, comes as zeros, and every lane loads, so that waits can count.
+  constexpr unsigned NOWHERE = 0x80000000u;
+  auto buffer = [](const void *at, int64_t bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(at), 0, (int)std::min<int64_t>(bytes, 0x7fffffff), 0x00020000);
   };
-  fetch_q(slot.begin);
+  constexpr bool Q_AHEAD = KS <= 6;   // (with wider heads the registers are full)
+  bf16x8 qf[KS], qn[Q_AHEAD ? KS : 1];
+  auto fetch_q = [&](int r0, bf16x8 (&to)[KS]) {   // rows past the end: the last one again
+    const int r = std::min(r0 + l32, slot.end - 1), q0 = std::min(r0, slot.end - 1) / p.group, q = r / p.group;
+    const __amdgpu_buffer_rsrc_t src = buffer(p.q + (slot.q_first + q0) * p.ld_q + h0 * p.dh, 0x7fffffff);
+    const unsigned at = ((unsigned)(q - q0) * (unsigned)p.ld_q + (unsigned)((r - q * p.group) * p.dh + 8 * lh)) * 2u;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+      to[ks] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(src, 2 * ks + lh < pieces ? at + ks * 32 : NOWHERE, 0, 0));
+  };
+  const int r_first = __builtin_amdgcn_readfirstlane(slot.begin + wave * 32);   // this wavefront's rows of the first row tile
+  if constexpr (Q_AHEAD) fetch_q(r_first, qn);
 
-  const int64_t kv_at = (int64_t)slot.kv_begin * p.ld_kv + blockIdx.y * p.dh;
+  const int64_t kv_at = (int64_t)slot.kv_begin * p.ld_kv + kv_head * p.dh;
   const bf16_t *const kbase = p.k + kv_at, *const vbase = p.v + kv_at;
-  const uint8_t *const mask = p.mask ? p.mask + slot.kv_begin : nullptr;
   struct Pieces { uintx4 k[CJ], v[CJ]; uint64_t bits; };
+  unsigned piece_at[CJ];
+#pragma unroll
+  for (int j = 0; j < CJ; ++j) {
+    const int i = tid + 64 * NW * j, row = i / C::CH, c = i - row * C::CH;
+    piece_at[j] = row < KT && c < pieces ? ((unsigned)row * (unsigned)p.ld_kv + c * 8) * 2u : NOWHERE;
+  }
   auto fetch = [&](int tile, Pieces &x) {
+    const int left = std::min(n_keys - tile * KT, KT);
+    const int64_t bytes = ((int64_t)(left - 1) * p.ld_kv + p.dh) * 2, at = (int64_t)tile * KT * p.ld_kv;
+    const __amdgpu_buffer_rsrc_t ksrc = buffer(kbase + at, bytes), vsrc = buffer(vbase + at, bytes);
 #pragma unroll
     for (int j = 0; j < CJ; ++j) {
-      const int i = tid + 64 * NW * j, row = i / C::CH, c = i - row * C::CH, key = tile * KT + row;
-      x.k[j] = x.v[j] = uintx4{0u, 0u, 0u, 0u};
-      if (row < KT && c < pieces && key < n_keys) {
-        x.k[j] = *reinterpret_cast<const uintx4 *>(kbase + (int64_t)key * p.ld_kv + c * 8);
-        x.v[j] = *reinterpret_cast<const uintx4 *>(vbase + (int64_t)key * p.ld_kv + c * 8);
-      }
+      x.k[j] = __builtin_amdgcn_raw_buffer_load_b128(ksrc, piece_at[j], 0, 0);
+      x.v[j] = __builtin_amdgcn_raw_buffer_load_b128(vsrc, piece_at[j], 0, 0);
     }
-    const int key = tile * KT + lane;
-    x.bits = __ballot(key < n_keys && (!mask || mask[key]));   // one bit a key
+    unsigned valid = lane < left;   // one bit a key
+    if (p.mask) valid = __builtin_amdgcn_raw_buffer_load_b8(buffer(p.mask + slot.kv_begin + tile * KT, left), lane, 0, 0);
+    x.bits = __ballot(valid != 0);
   };
   auto put = [&](int st, const Pieces &x) {
     unsigned char *const at = smem + st * C::STAGE;
@@ -146,48 +174,93 @@ __global__ __launch_bounds__(64 * NW) void k_cross_attn(CrossParams p) {
     }
     if (tid == 0) reinterpret_cast<uint64_t *>(smem + ST * C::STAGE)[st] = x.bits;
   };
+
   floatx16 o[C::DT];
   float m_run, l_run;
-  bf16x8 qf[KS];
   // transposing reads: this lane supplies the 8 bytes of key tr_key at feature tr_d of a 16 keys x 32 features block
   const int tr = C::VOFF + (4 * lh + ((lane & 15) >> 2)) * C::VP + (16 * ((lane >> 4) & 1) + 4 * (lane & 3)) * 2;
-  auto begin = [&]() {
+  auto begin = [&](int r0) {
+    if constexpr (Q_AHEAD) {
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) qf[ks] = qn[ks];
+      for (int ks = 0; ks < KS; ++ks) qf[ks] = qn[ks];
+      fetch_q(r0 + QT, qn);
+    } else {
+      fetch_q(r0, qf);
+    }
 #pragma unroll
     for (int d = 0; d < C::DT; ++d)
 #pragma unroll
       for (int e = 0; e < 16; ++e) o[d][e] = 0.f;
     m_run = -INFINITY; l_run = 0.f;
   };
-  auto step = [&](int st) {
-    const unsigned char *const at = smem + st * C::STAGE;
-    floatx16 s[2];
+  // Where a tile's fragments lie: K of key 32 (q % 2) + l32, k-step q / 2
+  auto k_frag = [&](int st, int q) {
+    return *reinterpret_cast<const bf16x8 *>(smem + st * C::STAGE + ((q & 1) * 32 + l32) * C::KP + (2 * (q >> 1) + lh) * 16);
+  };
+  auto valid_of = [&](int st, unsigned (&w)[2]) {
+    const uint64_t bits = reinterpret_cast<const uint64_t *>(smem + ST * C::STAGE)[st];
+    w[0] = (unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)bits);
+    w[1] = (unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)(bits >> 32));
+  };
+  constexpr int NQ = 2 * KS, NPV = 4 * C::DT;   // matrix instructions of a tile's scores and of its share of O
+  auto scores = [&](int st, floatx16 (&s)[2]) {
 #pragma unroll
-    for (int kt = 0; kt < 2; ++kt) {
+    for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
       for (int e = 0; e < 16; ++e) s[kt][e] = 0.f;
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks)
-        s[kt] = mfma32(*reinterpret_cast<const bf16x8 *>(at + (kt * 32 + l32) * C::KP + (2 * ks + lh) * 16), qf[ks], s[kt]);
+    for (int q = 0; q < NQ; ++q) s[q & 1] = mfma32(k_frag(st, q), qf[q >> 1], s[q & 1]);
+  };
+#define XA_FENCE() __builtin_amdgcn_sched_barrier(0)
+  // One tile: softmax of its scores and O^T += V^T P^T, with the next tile's scores formed on the way.  A wavefront issues in order, so the
+  // matrix instructions are threaded by hand through the vector arithmetic, which takes longer than they do: one after every two
+  // exponentials, the next tile's scores first, then those of O whose 16 keys' weights are there.  K fragments are read four instructions
+  // ahead, V fragments a chunk of 16 keys ahead.
+  auto step = [&](auto next_tag, int st, int st_next, floatx16 (&s)[2], floatx16 (&s_next)[2]) {
+    constexpr bool NEXT = decltype(next_tag)::value;
+    constexpr int KD = 4, NS = NEXT ? NQ : 0, M = NS + NPV;
+    bf16x8 kf[KD];
+    if constexpr (NEXT) {
+#pragma unroll
+      for (int q = 0; q < KD; ++q) kf[q] = k_frag(st_next, q);
     }
-    const uint64_t bits = reinterpret_cast<const uint64_t *>(smem + ST * C::STAGE)[st];
-    const unsigned lo_bits = (unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)bits);
-    const unsigned hi_bits = (unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)(bits >> 32));
-    if ((lo_bits & hi_bits) != ~0u) {
+    floatx16 zero;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) zero[e] = 0.f;
+    unsigned valid[2];
+    valid_of(st, valid);
+    if ((valid[0] & valid[1]) != ~0u) {
 #pragma unroll
       for (int kt = 0; kt < 2; ++kt) {
-        const unsigned w = (kt ? hi_bits : lo_bits) >> (4 * lh);
+        const int w = (int)(valid[kt] >> (4 * lh));
 #pragma unroll
-        for (int e = 0; e < 16; ++e) s[kt][e] = (w >> (8 * (e >> 2) + (e & 3))) & 1u ? s[kt][e] : -INFINITY;
+        for (int e = 0; e < 16; ++e) {
+          const int keep = __builtin_amdgcn_sbfe(w, 8 * (e >> 2) + (e & 3), 1);   // all ones or none
+          s[kt][e] = __int_as_float((__float_as_int(s[kt][e]) & keep) | (0xff800000 & ~keep));
+        }
       }
     }
-    float mx = s[0][0];
+    XA_FENCE();
+#define XA_SLOT_QK(Q)                                                       \
+  do {                                                                      \
+    s_next[(Q) & 1] = mfma32(kf[(Q) % KD], qf[(Q) >> 1], (Q) < 2 ? zero : s_next[(Q) & 1]);  \
+    if ((Q) + KD < NQ) kf[(Q) % KD] = k_frag(st_next, (Q) + KD);            \
+  } while (0)
+    int slot = 0;
+    if constexpr (NEXT) { XA_SLOT_QK(0); slot = 1; }
+    XA_FENCE();
+    float mx = fmaxf(s[0][0], s[0][1]);
 #pragma unroll
-    for (int e = 1; e < 16; ++e) mx = fmaxf(mx, s[0][e]);
+    for (int e = 2; e < 16; ++e) mx = fmaxf(mx, s[0][e]);
+    XA_FENCE();
+    if constexpr (NEXT) { XA_SLOT_QK(1); slot = 2; }
+    XA_FENCE();
 #pragma unroll
     for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[1][e]);
-    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+    XA_FENCE();
+    if constexpr (NEXT) { XA_SLOT_QK(2); slot = 3; }
+    const Swapped both = swap_halves(__float_as_uint(mx), __float_as_uint(mx));
+    mx = fmaxf(__uint_as_float(both.a), __uint_as_float(both.b));
     const bool move = mx > m_run + p.rebase;
     if (__ballot(move)) {
       const float alpha = move ? __builtin_amdgcn_exp2f((m_run - mx) * p.scale_log2) : 1.f;   // 0 the first time
@@ -199,35 +272,65 @@ __global__ __launch_bounds__(64 * NW) void k_cross_attn(CrossParams p) {
         for (int e = 0; e < 16; ++e) o[d][e] *= alpha;
     }
     const float ref = m_run == -INFINITY ? 0.f : m_run * p.scale_log2;
-    bf16x8 pf[4];
-    float sum = 0.f;
-#pragma unroll
-    for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kt][e], p.scale_log2, -ref));
-        sum += w;
-        pf[2 * kt + (e >> 3)][e & 7] = (bf16_t)w;
-      }
-    l_run += sum;
-#pragma unroll
-    for (int kc = 0; kc < 4; ++kc)
+    const unsigned char *const va = smem + st * C::STAGE + tr;
+    bf16x8 pf[4], vf[2][C::DT];
+    auto v_frags = [&](int kc) {
 #pragma unroll
       for (int d = 0; d < C::DT; ++d) {
-        const unsigned char *const va = at + tr + kc * 16 * C::VP + d * 64;
-        const shortx4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4_ptr_t)va);
-        const shortx4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4_ptr_t)(va + 8 * C::VP));
-        o[d] = mfma32(__builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7)), pf[kc], o[d]);
+        const shortx4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4_ptr_t)(va + kc * 16 * C::VP + d * 64));
+        const shortx4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4_ptr_t)(va + (kc * 16 + 8) * C::VP + d * 64));
+        vf[kc & 1][d] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
       }
+    };
+    v_frags(0);
+    XA_FENCE();
+    float sum = 0.f;
+#pragma unroll
+    for (int g = 0; g < 16; ++g) {
+#pragma unroll
+      for (int e = 2 * g; e < 2 * g + 2; ++e) {
+        const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e >> 4][e & 15], p.scale_log2, -ref));
+        sum += w;
+        pf[e >> 3][e & 7] = (bf16_t)w;
+      }
+      XA_FENCE();
+      if (slot < NS) {
+        if constexpr (NEXT) XA_SLOT_QK(slot);
+        ++slot;
+      } else if (slot < M) {
+        const int v = slot - NS, kc = v / C::DT, d = v - kc * C::DT;
+        if (g >= 4 * kc + 3) {
+          if (d == 0 && kc < 3) v_frags(kc + 1);
+          o[d] = mfma32(vf[kc & 1][d], pf[kc], o[d]);
+          ++slot;
+        }
+      }
+      XA_FENCE();
+    }
+#pragma unroll
+    for (int sl = 0; sl < M; ++sl)
+      if (sl >= slot) {
+        if (sl < NS) {
+          if constexpr (NEXT) XA_SLOT_QK(sl);
+        } else {
+          const int v = sl - NS, kc = v / C::DT, d = v - kc * C::DT;
+          if (d == 0 && kc < 3) v_frags(kc + 1);
+          o[d] = mfma32(vf[kc & 1][d], pf[kc], o[d]);
+        }
+      }
+    l_run += sum;
+#undef XA_SLOT_QK
   };
+  using Yes = std::true_type;
+  using No = std::false_type;
   auto finish = [&](int r0) {
-    const int r = r0 + wave * 32 + l32, q = r / p.group, h = h0 + r - q * p.group;
+    const int r = r0 + l32, q = r / p.group, h = h0 + r - q * p.group;
     const bool in = r < slot.end;
     const int64_t token = slot.q_first + q;
     l_run += __shfl_xor(l_run, 32, 64);
     if (p.parts > 1) {
       if (in) {
-        const int64_t at = (blockIdx.z * (int64_t)p.q_rows + token) * p.H + h;
+        const int64_t at = (part * (int64_t)p.q_rows + token) * p.H + h;
 #pragma unroll
         for (int d = 0; d < C::DT; ++d)
 #pragma unroll
@@ -244,59 +347,91 @@ __global__ __launch_bounds__(64 * NW) void k_cross_attn(CrossParams p) {
       }
       return;
     }
+    // Lanes without a row, or past the head dim, store past the end of the buffer, which drops it: the same stores for every tile, so that
+    // the wait for the next queries, which were asked for before them, need not be one for all stores.
     const float inv = l_run == 0.f ? 0.f : 1.f / l_run;
-    bf16_t *const orow = p.o + token * p.ld_o + h * p.dh;
+    const int q0 = r0 / p.group;   // first token of the tile
+    const __amdgpu_buffer_rsrc_t r_o = buffer(p.o + (slot.q_first + q0) * p.ld_o + h0 * p.dh, 0x7fffffff);
+    const unsigned o_at = in ? ((unsigned)(q - q0) * (unsigned)p.ld_o + (unsigned)((h - h0) * p.dh)) * 2u : NOWHERE;
+    // Of 32 features lanes l and l + 32 hold groups of four in turn.  Two exchanges make it four lanes a row with eight features each, so that
+    // a store writes 64 bytes of 16 rows (with 32 bytes of 32 rows 97200 queries of one state took 150 us, without storing 88).
+    const unsigned at_lo = (unsigned)__shfl((int)o_at, lane & 15, 64), at_hi = (unsigned)__shfl((int)o_at, 16 + (lane & 15), 64);
+    const int col_lane = 8 * (2 * ((lane >> 4) & 1) + lh);
 #pragma unroll
-    for (int d = 0; d < C::DT; ++d)
+    for (int d = 0; d < C::DT; ++d) {
+      uintx4 v[2];
 #pragma unroll
-      for (int g = 0; g < 4; g += 2) {
-        // lanes l and l ^ 32 hold the two halves of 8 features each: the lower lane collects those of group g, the upper those of g + 1
+      for (int i = 0; i < 2; ++i) {
         bf16x4 x0, x1;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) { x0[e] = (bf16_t)(o[d][4 * g + e] * inv); x1[e] = (bf16_t)(o[d][4 * g + 4 + e] * inv); }
-        const uintx2 own = __builtin_bit_cast(uintx2, lh ? x1 : x0), give = __builtin_bit_cast(uintx2, lh ? x0 : x1);
-        uintx2 got;
-        got[0] = (unsigned)__shfl_xor((int)give[0], 32, 64);
-        got[1] = (unsigned)__shfl_xor((int)give[1], 32, 64);
-        const uintx4 v = lh ? uintx4{got[0], got[1], own[0], own[1]} : uintx4{own[0], own[1], got[0], got[1]};
-        const int col = 32 * d + 8 * (g + lh);
-        if (in && col < p.dh) *reinterpret_cast<uintx4 *>(orow + col) = v;
+        for (int e = 0; e < 4; ++e) { x0[e] = (bf16_t)(o[d][8 * i + e] * inv); x1[e] = (bf16_t)(o[d][8 * i + 4 + e] * inv); }
+        const uintx2 y0 = __builtin_bit_cast(uintx2, x0), y1 = __builtin_bit_cast(uintx2, x1);
+        const Swapped w0 = swap_halves(y0[0], y1[0]), w1 = swap_halves(y0[1], y1[1]);
+        v[i] = uintx4{w0.a, w1.a, w0.b, w1.b};
       }
-    if (p.lse && lh == 0 && in)
-      p.lse[token * p.H + h] = l_run == 0.f ? -INFINITY : __builtin_fmaf(m_run, p.scale, __builtin_amdgcn_logf(l_run) * 0.6931471805599453f);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const Swapped w = swap_quarters(v[0][i], v[1][i]);
+        v[0][i] = w.a; v[1][i] = w.b;
+      }
+      const int col = 32 * d + col_lane;
+      const bool is = col < p.dh;
+      __builtin_amdgcn_raw_buffer_store_b128(v[0], r_o, is && at_lo != NOWHERE ? at_lo + col * 2u : NOWHERE, 0, 0);
+      __builtin_amdgcn_raw_buffer_store_b128(v[1], r_o, is && at_hi != NOWHERE ? at_hi + col * 2u : NOWHERE, 0, 0);
+    }
+    if (p.lse) {
+      const __amdgpu_buffer_rsrc_t r_l = buffer(p.lse + (int64_t)(slot.q_first + q0) * p.H + h0, 0x7fffffff);
+      const float v = l_run == 0.f ? -INFINITY : __builtin_fmaf(m_run, p.scale, __builtin_amdgcn_logf(l_run) * 0.6931471805599453f);
+      __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v), r_l, in && lh == 0 ? ((unsigned)(q - q0) * p.H + (h - h0)) * 4u : NOWHERE, 0, 0);
+    }
   };
 
   if (n_tiles <= ST) {
-    // everything is fetched once, and the workgroup walks over its row tiles with no further barrier
-    {
-      Pieces x[ST];
+    // everything is fetched once, and every wavefront walks over its row tiles with no further barrier
+    constexpr int FLY = NW == 1 ? 1 : ST;   // tiles in registers at a time
 #pragma unroll
-      for (int t = 0; t < ST; ++t)
-        if (t < n_tiles) fetch(t_begin + t, x[t]);
+    for (int t0 = 0; t0 < ST; t0 += FLY) {
+      Pieces x[FLY];
 #pragma unroll
-      for (int t = 0; t < ST; ++t)
-        if (t < n_tiles) put(t, x[t]);
+      for (int t = 0; t < FLY; ++t)
+        if (t0 + t < n_tiles) fetch(t_begin + t0 + t, x[t]);
+#pragma unroll
+      for (int t = 0; t < FLY; ++t)
+        if (t0 + t < n_tiles) put(t0 + t, x[t]);
     }
     __syncthreads();
-    for (int r0 = slot.begin; r0 < slot.end; r0 += QT) {
-      begin();
-      if (r0 + QT < slot.end) fetch_q(r0 + QT);
-      if (r0 + wave * 32 >= slot.end) break;   // a wavefront without rows, in the run's last tile
-      for (int t = 0; t < n_tiles; ++t) step(t);
+    for (int r0 = r_first; r0 < slot.end; r0 += QT) {
+      begin(r0);
+      if (n_tiles > 0) {
+        floatx16 s0[2], s1[2];
+        scores(0, s0);
+        int t = 0;
+        for (; t + 2 < n_tiles; t += 2) {
+          step(Yes{}, t, t + 1, s0, s1);
+          step(Yes{}, t + 1, t + 2, s1, s0);
+        }
+        if (t + 2 == n_tiles) {
+          step(Yes{}, t, t + 1, s0, s1);
+          step(No{}, t + 1, 0, s1, s0);
+        } else {
+          step(No{}, t, 0, s0, s1);
+        }
+      }
       finish(r0);
     }
   } else {
-    for (int r0 = slot.begin; r0 < slot.end; r0 += QT) {
+    for (int r0 = r_first; r0 - wave * 32 < slot.end; r0 += QT) {   // wavefronts without rows come along for the barriers
       Pieces x;
-      begin();
-      if (r0 + QT < slot.end) fetch_q(r0 + QT);
+      begin(r0);
       fetch(t_begin, x);
-      if (r0 != slot.begin) __syncthreads();   // the tiles of the rows before are done with
+      if (r0 != r_first) __syncthreads();   // the tiles of the rows before are done with
       put(0, x);
       __syncthreads();
       for (int t = 0; t < n_tiles; ++t) {
         if (t + 1 < n_tiles) fetch(t_begin + t + 1, x);
-        step(t & 1);
+        floatx16 sc[2], none[2];
+        scores(t & 1, sc);
+        step(No{}, t & 1, 0, sc, none);
         if (t + 1 < n_tiles) put((t + 1) & 1, x);
         __syncthreads();
       }
@@ -345,30 +480,31 @@ int launch_as(const CrossParams &p, hipStream_t s) {
   const int rc = ddit::allow_dynamic_lds(reinterpret_cast<const void *>(&k_cross_attn<KS, NW, ST>), smem, &allowed);
   if (rc != 0) return rc;
   const unsigned slots = (unsigned)((int64_t)p.q_rows * p.group / p.run + p.B);
-  hipLaunchKernelGGL((k_cross_attn<KS, NW, ST>), dim3(slots, (unsigned)(p.H / p.group), (unsigned)p.parts), dim3(64 * NW), smem, s, p);
+  const int64_t blocks = (int64_t)((slots + 7) / 8 * 8) * (p.H / p.group) * p.parts;
+  if (blocks > 0x7fffffff) { ddit::set_error("packed cross-attention: too many workgroups"); return -2; }
+  hipLaunchKernelGGL((k_cross_attn<KS, NW, ST>), dim3((unsigned)blocks), dim3(64 * NW), smem, s, p);
   return ddit::hip_fail(hipGetLastError(), "packed cross-attention launch");
 }
 template <int KS>
 int launch_form(int waves, const CrossParams &p, hipStream_t s) {
   if (waves == 1) return launch_as<KS, 1, 2>(p, s);
-  if (waves == 4) return launch_as<KS, 4, 2>(p, s);
   return launch_as<KS, 8, KS == 8 ? 4 : 5>(p, s);
 }
 
-// Wavefronts of a workgroup, for `rows` rows a key head
-int waves_for(int B, int64_t rows, int H_kv) {
-  if (rows <= (int64_t)64 * B) return 1;
-  return (rows / 256 + B) * H_kv >= 1024 ? 8 : 4;
-}
+// Wavefronts of a workgroup, for `rows` rows a key head: one where sequences have few, on average
+int waves_for(int B, int64_t rows) { return rows <= (int64_t)64 * B ? 1 : 8; }
 
 }  // namespace
 
 namespace ddit {
 
-// From the totals alone, since the lengths are on the device, and for the whole chip whatever device is current, since the answer sizes workspaces.
+// From the totals alone, since the lengths are on the device, and for the whole chip whatever device is current, since the answer sizes workspaces:
+// parts of 128 keys and more, as many as make one round of the chip (a workgroup of eight wavefronts fills a CU, four of one do).
 int cross_attn_parts(int B, int64_t q_rows, int64_t kv_rows, int H, int H_kv) {
-  const int64_t rows = q_rows * (H / H_kv), units = (rows / (32 * waves_for(B, rows, H_kv)) + B) * H_kv;
-  return (int)std::max<int64_t>(1, std::min<int64_t>({(int64_t)32, 1024 / units, kv_rows / 128}));
+  const int64_t rows = q_rows * (H / H_kv);
+  const int waves = waves_for(B, rows);
+  const int64_t units = (rows / (32 * waves) + B) * H_kv;
+  return (int)std::max<int64_t>(1, std::min<int64_t>({(int64_t)32, (waves == 1 ? 1024 : 256) / units, kv_rows / 128}));
 }
 
 int launch_cross_attn(const CrossAttnArgs &a, hipStream_t s) {
@@ -383,9 +519,17 @@ int launch_cross_attn(const CrossAttnArgs &a, hipStream_t s) {
   p.part_o = a.scratch;
   p.part_ml = p.parts > 1 ? a.scratch + (int64_t)p.parts * a.q_rows * a.H * a.dh : nullptr;
   const int64_t rows = a.q_rows * p.group;
-  const int waves = waves_for(a.B, rows, a.H_kv);
+  const int waves = waves_for(a.B, rows);
   p.run = 32 * waves;
-  if (waves == 8) p.run *= (int)std::max<int64_t>(1, std::min<int64_t>(8, rows * a.H_kv / (256 * 4 * device_cus())));
+  if (waves == 8 && p.parts == 1) {
+    // row tiles a workgroup walks over: a round of the chip takes that many and about one more for its set-up; counted for sequences of one length
+    int64_t best = 0, cost = INT64_MAX;
+    for (int64_t m = 1; m <= 16; ++m) {
+      const int64_t blocks = a.B * ((rows + a.B * 256 * m - 1) / (a.B * 256 * m)) * a.H_kv, c = (blocks + device_cus() - 1) / device_cus() * (m + 1);
+      if (c < cost) { cost = c; best = m; }
+    }
+    p.run *= (int)best;
+  }
   const int rc = p.dh <= 64 ? launch_form<4>(waves, p, s) : p.dh <= 80 ? launch_form<5>(waves, p, s) : p.dh <= 96 ? launch_form<6>(waves, p, s)
                                                                                                               : launch_form<8>(waves, p, s);
   if (rc != 0 || p.parts == 1) return rc;

@@ -1051,6 +1051,9 @@ int ddit_cross_attn_packed_fwd(const void *q, int64_t ld_q, const int32_t *q_off
     return DDIT_ERR_INVALID_ARG;
   }
   if (ld_q % 8 || ld_kv % 8 || ld_o % 8) { set_error("leading dimensions must be multiples of 8"); return DDIT_ERR_ALIGNMENT; }
+  if (ld_q >= 1 << 22 || ld_kv >= 1 << 22 || ld_o >= 1 << 22) {
+    set_error("leading dimensions (%lld,%lld,%lld): below 2^22 are supported", (long long)ld_q, (long long)ld_kv, (long long)ld_o); return DDIT_ERR_UNSUPPORTED;
+  }
   for (const void *a : {q, k, v, (const void *)o})
     if (!aligned16(a)) { set_error("q, k, v and o must be 16-byte aligned"); return DDIT_ERR_ALIGNMENT; }
   for (const void *a : {(const void *)q_offsets, (const void *)kv_offsets, (const void *)lse_or_null})

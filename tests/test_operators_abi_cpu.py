@@ -108,7 +108,7 @@ def test_cross_packed_refusals(m):
                 dict(G=0), dict(G=3), dict(dh=0), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")), dict(ld_q=248),
                 dict(ld_kv=120), dict(ld_o=248)):
         assert call(**bad) == -1, bad
-    for bad in (dict(dh=60), dict(dh=136, ld_q=1024, ld_kv=1024, ld_o=1024), dict(B=1 << 20), dict(q_rows=1 << 31), dict(kv_rows=1 << 31), dict(H=1 << 17)):
+    for bad in (dict(dh=60), dict(dh=136, ld_q=1024, ld_kv=1024, ld_o=1024), dict(B=1 << 20), dict(q_rows=1 << 31), dict(kv_rows=1 << 31), dict(H=1 << 17), dict(ld_o=1 << 22), dict(ld_q=1 << 22), dict(ld_kv=1 << 22)):
         assert call(**bad) == -2, bad
     for bad in (dict(ld_q=260), dict(ld_kv=132), dict(ld_o=260), dict(q=P(0x1008)), dict(k=P(0x3008)), dict(v=P(0x4002)), dict(o=P(0x6008)), dict(q_off=P(0x2002)),
                 dict(kv_off=P(0x5001)), dict(lse=P(0x8002))):
