@@ -105,7 +105,8 @@ struct CrossCfg {
   static_assert(DT * 64 <= VP && SMEM <= 160 * 1024, "a V row is read to the end of its last tile");
 };
 
-template <int KS, int NW, int ST>
+// PARTS: a part of the keys, whose sums go to part_o and part_ml
+template <int KS, int NW, int ST, bool PARTS>
 __global__ __launch_bounds__(64 * NW) void k_cross_attn(CrossParams p) {
   using C = CrossCfg<KS, ST>;
   constexpr int QT = 32 * NW, CJ = (KT * C::CH + 64 * NW - 1) / (64 * NW);   // pieces of a tile that a thread stages
@@ -114,12 +115,12 @@ __global__ __launch_bounds__(64 * NW) void k_cross_attn(CrossParams p) {
   // Workgroups are dealt out to the 8 XCDs in turn.  The heads of a slot come one after the other on one XCD: a row of one head is 2 dh bytes
   // of the token's, so heads share the cache lines of q and o, which its L2 puts together.
   const int H_kv = p.H / p.group, i0 = blockIdx.x >> 3, i1 = i0 / H_kv, kv_head = i0 - i1 * H_kv;
-  const int i2 = i1 / p.parts, part = i1 - i2 * p.parts;
+  const int i2 = PARTS ? i1 / p.parts : i1, part = PARTS ? i1 - i2 * p.parts : 0;
   Slot slot;
   if (!find_slot(p, (unsigned)i2 * 8 + (blockIdx.x & 7), p.run, slot)) return;
   const int h0 = kv_head * p.group;   // first of the key head's query heads
   const int n_keys = slot.kv_end - slot.kv_begin, all = (n_keys + KT - 1) / KT;
-  const int t_begin = (int)((int64_t)all * part / p.parts), t_end = (int)((int64_t)all * (part + 1) / p.parts);
+  const int t_begin = PARTS ? (int)((int64_t)all * part / p.parts) : 0, t_end = PARTS ? (int)((int64_t)all * (part + 1) / p.parts) : all;
   const int n_tiles = t_end - t_begin, pieces = p.dh >> 3;
 
   // Everything is loaded through buffers: what lies past an end, or is sent there, comes as zeros, and every lane loads, so that waits can count.
@@ -328,7 +329,7 @@ __global__ __launch_bounds__(64 * NW) void k_cross_attn(CrossParams p) {
     const bool in = r < slot.end;
     const int64_t token = slot.q_first + q;
     l_run += __shfl_xor(l_run, 32, 64);
-    if (p.parts > 1) {
+    if constexpr (PARTS) {
       if (in) {
         const int64_t at = (part * (int64_t)p.q_rows + token) * p.H + h;
 #pragma unroll
@@ -379,11 +380,9 @@ __global__ __launch_bounds__(64 * NW) void k_cross_attn(CrossParams p) {
       __builtin_amdgcn_raw_buffer_store_b128(v[0], r_o, is && at_lo != NOWHERE ? at_lo + col * 2u : NOWHERE, 0, 0);
       __builtin_amdgcn_raw_buffer_store_b128(v[1], r_o, is && at_hi != NOWHERE ? at_hi + col * 2u : NOWHERE, 0, 0);
     }
-    if (p.lse) {
-      const __amdgpu_buffer_rsrc_t r_l = buffer(p.lse + (int64_t)(slot.q_first + q0) * p.H + h0, 0x7fffffff);
-      const float v = l_run == 0.f ? -INFINITY : __builtin_fmaf(m_run, p.scale, __builtin_amdgcn_logf(l_run) * 0.6931471805599453f);
-      __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v), r_l, in && lh == 0 ? ((unsigned)(q - q0) * p.H + (h - h0)) * 4u : NOWHERE, 0, 0);
-    }
+    const __amdgpu_buffer_rsrc_t r_l = buffer(p.lse ? p.lse + (int64_t)(slot.q_first + q0) * p.H + h0 : nullptr, p.lse ? 0x7fffffff : 0);
+    const float lse = l_run == 0.f ? -INFINITY : __builtin_fmaf(m_run, p.scale, __builtin_amdgcn_logf(l_run) * 0.6931471805599453f);
+    __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(lse), r_l, in && lh == 0 ? ((unsigned)(q - q0) * p.H + (h - h0)) * 4u : NOWHERE, 0, 0);
   };
 
   if (n_tiles <= ST) {
@@ -473,22 +472,23 @@ __global__ __launch_bounds__(256) void k_cross_join(CrossParams p) {
   if (p.lse && lane == 0) p.lse[at] = l == 0.f ? -INFINITY : __builtin_fmaf(top, p.scale, __builtin_amdgcn_logf(l) * 0.6931471805599453f);
 }
 
-template <int KS, int NW, int ST>
+template <int KS, int NW, int ST, bool PARTS>
 int launch_as(const CrossParams &p, hipStream_t s) {
   constexpr int smem = CrossCfg<KS, ST>::SMEM;
   static std::atomic<uint64_t> allowed;
-  const int rc = ddit::allow_dynamic_lds(reinterpret_cast<const void *>(&k_cross_attn<KS, NW, ST>), smem, &allowed);
+  const int rc = ddit::allow_dynamic_lds(reinterpret_cast<const void *>(&k_cross_attn<KS, NW, ST, PARTS>), smem, &allowed);
   if (rc != 0) return rc;
   const unsigned slots = (unsigned)((int64_t)p.q_rows * p.group / p.run + p.B);
   const int64_t blocks = (int64_t)((slots + 7) / 8 * 8) * (p.H / p.group) * p.parts;
   if (blocks > 0x7fffffff) { ddit::set_error("packed cross-attention: too many workgroups"); return -2; }
-  hipLaunchKernelGGL((k_cross_attn<KS, NW, ST>), dim3((unsigned)blocks), dim3(64 * NW), smem, s, p);
+  hipLaunchKernelGGL((k_cross_attn<KS, NW, ST, PARTS>), dim3((unsigned)blocks), dim3(64 * NW), smem, s, p);
   return ddit::hip_fail(hipGetLastError(), "packed cross-attention launch");
 }
 template <int KS>
 int launch_form(int waves, const CrossParams &p, hipStream_t s) {
-  if (waves == 1) return launch_as<KS, 1, 2>(p, s);
-  return launch_as<KS, 8, KS == 8 ? 4 : 5>(p, s);
+  constexpr int ST = KS == 8 ? 4 : 5;   // as many stages as the LDS holds
+  if (waves == 1) return p.parts > 1 ? launch_as<KS, 1, 2, true>(p, s) : launch_as<KS, 1, 2, false>(p, s);
+  return p.parts > 1 ? launch_as<KS, 8, ST, true>(p, s) : launch_as<KS, 8, ST, false>(p, s);
 }
 
 // Wavefronts of a workgroup, for `rows` rows a key head: one where sequences have few, on average
