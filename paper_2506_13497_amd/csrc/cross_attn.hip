@@ -99,8 +99,8 @@ struct CrossCfg {
   static constexpr int DT = (KS + 1) / 2;            // 32-row tiles of V^T
   static constexpr int KP = CH * 16 + 16;            // K row pitch: an odd number of pieces, so 16 rows lie in different banks
   static constexpr int VP = KS == 8 ? 320 : 192;     // V row pitch: an odd number of 64 bytes, so the four keys of a transposing read do
-  static constexpr int VOFF = KT * KP;
-  static constexpr int STAGE = KT * (KP + VP);
+  static constexpr int VOFF = ST == 1 ? 0 : KT * KP; // (with one stage K stays in registers)
+  static constexpr int STAGE = VOFF + KT * VP;
   static constexpr int SMEM = ST * STAGE + ST * 8;   // and the valid keys of every stage
   static_assert(DT * 64 <= VP && SMEM <= 160 * 1024, "a V row is read to the end of its last tile");
 };
@@ -128,7 +128,7 @@ __global__ __launch_bounds__(64 * NW) void k_cross_attn(CrossParams p) {
   auto buffer = [](const void *at, int64_t bytes) {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(at), 0, (int)std::min<int64_t>(bytes, 0x7fffffff), 0x00020000);
   };
-  constexpr bool Q_AHEAD = KS <= 6;   // (with wider heads the registers are full)
+  constexpr bool Q_AHEAD = NW > 1 && KS <= 6;   // (with wider heads the registers are full)
   bf16x8 qf[KS], qn[Q_AHEAD ? KS : 1];
   auto fetch_q = [&](int r0, bf16x8 (&to)[KS]) {   // rows past the end: the last one again
     const int r = std::min(r0 + l32, slot.end - 1), q0 = std::min(r0, slot.end - 1) / p.group, q = r / p.group;
@@ -143,20 +143,29 @@ __global__ __launch_bounds__(64 * NW) void k_cross_attn(CrossParams p) {
 
   const int64_t kv_at = (int64_t)slot.kv_begin * p.ld_kv + kv_head * p.dh;
   const bf16_t *const kbase = p.k + kv_at, *const vbase = p.v + kv_at;
-  struct Pieces { uintx4 k[CJ], v[CJ]; uint64_t bits; };
+  // What a thread holds of a tile: pieces to stage of K and V, or, where a wavefront is alone, its K fragments as they are.
+  constexpr bool ALONE = NW == 1;
+  constexpr int NQ = 2 * KS, NPV = 4 * C::DT;   // matrix instructions of a tile's scores and of its share of O
+  struct Pieces { uintx4 k[ALONE ? NQ : CJ], v[CJ]; uint64_t bits; };
   unsigned piece_at[CJ];
 #pragma unroll
   for (int j = 0; j < CJ; ++j) {
     const int i = tid + 64 * NW * j, row = i / C::CH, c = i - row * C::CH;
     piece_at[j] = row < KT && c < pieces ? ((unsigned)row * (unsigned)p.ld_kv + c * 8) * 2u : NOWHERE;
   }
+  const unsigned frag_at = ((unsigned)l32 * (unsigned)p.ld_kv + 8 * lh) * 2u;
   auto fetch = [&](int tile, Pieces &x) {
     const int left = std::min(n_keys - tile * KT, KT);
     const int64_t bytes = ((int64_t)(left - 1) * p.ld_kv + p.dh) * 2, at = (int64_t)tile * KT * p.ld_kv;
     const __amdgpu_buffer_rsrc_t ksrc = buffer(kbase + at, bytes), vsrc = buffer(vbase + at, bytes);
+    if constexpr (ALONE) {
+#pragma unroll
+      for (int q = 0; q < NQ; ++q)   // key 32 (q % 2) + l32, k-step q / 2
+        x.k[q] = __builtin_amdgcn_raw_buffer_load_b128(ksrc, 2 * (q >> 1) + lh < pieces ? frag_at + (q >> 1) * 32 : NOWHERE, (q & 1) * 64 * (int)p.ld_kv, 0);
+    }
 #pragma unroll
     for (int j = 0; j < CJ; ++j) {
-      x.k[j] = __builtin_amdgcn_raw_buffer_load_b128(ksrc, piece_at[j], 0, 0);
+      if constexpr (!ALONE) x.k[j] = __builtin_amdgcn_raw_buffer_load_b128(ksrc, piece_at[j], 0, 0);
       x.v[j] = __builtin_amdgcn_raw_buffer_load_b128(vsrc, piece_at[j], 0, 0);
     }
     unsigned valid = lane < left;   // one bit a key
@@ -169,11 +178,11 @@ __global__ __launch_bounds__(64 * NW) void k_cross_attn(CrossParams p) {
     for (int j = 0; j < CJ; ++j) {
       const int i = tid + 64 * NW * j, row = i / C::CH, c = i - row * C::CH;
       if (row < KT) {
-        *reinterpret_cast<uintx4 *>(at + row * C::KP + c * 16) = x.k[j];   // zeros past the head dim
+        if constexpr (!ALONE) *reinterpret_cast<uintx4 *>(at + row * C::KP + c * 16) = x.k[j];   // zeros past the head dim
         *reinterpret_cast<uintx4 *>(at + C::VOFF + row * C::VP + c * 16) = (x.bits >> row) & 1 ? x.v[j] : uintx4{0u, 0u, 0u, 0u};
       }
     }
-    if (tid == 0) reinterpret_cast<uint64_t *>(smem + ST * C::STAGE)[st] = x.bits;
+    if (!ALONE && tid == 0) reinterpret_cast<uint64_t *>(smem + ST * C::STAGE)[st] = x.bits;
   };
 
   floatx16 o[C::DT];
@@ -198,12 +207,7 @@ __global__ __launch_bounds__(64 * NW) void k_cross_attn(CrossParams p) {
   auto k_frag = [&](int st, int q) {
     return *reinterpret_cast<const bf16x8 *>(smem + st * C::STAGE + ((q & 1) * 32 + l32) * C::KP + (2 * (q >> 1) + lh) * 16);
   };
-  auto valid_of = [&](int st, unsigned (&w)[2]) {
-    const uint64_t bits = reinterpret_cast<const uint64_t *>(smem + ST * C::STAGE)[st];
-    w[0] = (unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)bits);
-    w[1] = (unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)(bits >> 32));
-  };
-  constexpr int NQ = 2 * KS, NPV = 4 * C::DT;   // matrix instructions of a tile's scores and of its share of O
+  auto valid_of = [&](int st) { return reinterpret_cast<const uint64_t *>(smem + ST * C::STAGE)[st]; };
   auto scores = [&](int st, floatx16 (&s)[2]) {
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt)
@@ -217,7 +221,7 @@ __global__ __launch_bounds__(64 * NW) void k_cross_attn(CrossParams p) {
   // matrix instructions are threaded by hand through the vector arithmetic, which takes longer than they do: one after every two
   // exponentials, the next tile's scores first, then those of O whose 16 keys' weights are there.  K fragments are read four instructions
   // ahead, V fragments a chunk of 16 keys ahead.
-  auto step = [&](auto next_tag, int st, int st_next, floatx16 (&s)[2], floatx16 (&s_next)[2]) {
+  auto step = [&](auto next_tag, int st, uint64_t bits, int st_next, floatx16 (&s)[2], floatx16 (&s_next)[2]) {
     constexpr bool NEXT = decltype(next_tag)::value;
     constexpr int KD = 4, NS = NEXT ? NQ : 0, M = NS + NPV;
     bf16x8 kf[KD];
@@ -228,8 +232,7 @@ __global__ __launch_bounds__(64 * NW) void k_cross_attn(CrossParams p) {
     floatx16 zero;
 #pragma unroll
     for (int e = 0; e < 16; ++e) zero[e] = 0.f;
-    unsigned valid[2];
-    valid_of(st, valid);
+    const unsigned valid[2] = {(unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)bits), (unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)(bits >> 32))};
     if ((valid[0] & valid[1]) != ~0u) {
 #pragma unroll
       for (int kt = 0; kt < 2; ++kt) {
@@ -385,18 +388,36 @@ __global__ __launch_bounds__(64 * NW) void k_cross_attn(CrossParams p) {
     __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(lse), r_l, in && lh == 0 ? ((unsigned)(q - q0) * p.H + (h - h0)) * 4u : NOWHERE, 0, 0);
   };
 
-  if (n_tiles <= ST) {
+  if constexpr (ALONE) {
+    // one wavefront, whose LDS operations stay in order: no barrier, one stage for V, and K straight into registers; the next tile is on its
+    // way during the softmax of this one
+    Pieces x;
+    if (n_tiles > 0) fetch(t_begin, x);
+    begin(r_first);
+    for (int t = 0; t < n_tiles; ++t) {
+      floatx16 sc[2], none[2];
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sc[kt][e] = 0.f;
+#pragma unroll
+      for (int q = 0; q < NQ; ++q) sc[q & 1] = mfma32(__builtin_bit_cast(bf16x8, x.k[q]), qf[q >> 1], sc[q & 1]);
+      put(0, x);
+      const uint64_t bits = x.bits;
+      if (t + 1 < n_tiles) fetch(t_begin + t + 1, x);
+      step(No{}, 0, bits, 0, sc, none);
+    }
+    finish(r_first);
+  } else if (n_tiles <= ST) {
     // everything is fetched once, and every wavefront walks over its row tiles with no further barrier
-    constexpr int FLY = NW == 1 ? 1 : ST;   // tiles in registers at a time
+    {
+      Pieces x[ST];
 #pragma unroll
-    for (int t0 = 0; t0 < ST; t0 += FLY) {
-      Pieces x[FLY];
+      for (int t = 0; t < ST; ++t)
+        if (t < n_tiles) fetch(t_begin + t, x[t]);
 #pragma unroll
-      for (int t = 0; t < FLY; ++t)
-        if (t0 + t < n_tiles) fetch(t_begin + t0 + t, x[t]);
-#pragma unroll
-      for (int t = 0; t < FLY; ++t)
-        if (t0 + t < n_tiles) put(t0 + t, x[t]);
+      for (int t = 0; t < ST; ++t)
+        if (t < n_tiles) put(t, x[t]);
     }
     __syncthreads();
     for (int r0 = r_first; r0 < slot.end; r0 += QT) {
@@ -406,14 +427,14 @@ __global__ __launch_bounds__(64 * NW) void k_cross_attn(CrossParams p) {
         scores(0, s0);
         int t = 0;
         for (; t + 2 < n_tiles; t += 2) {
-          step(Yes{}, t, t + 1, s0, s1);
-          step(Yes{}, t + 1, t + 2, s1, s0);
+          step(Yes{}, t, valid_of(t), t + 1, s0, s1);
+          step(Yes{}, t + 1, valid_of(t + 1), t + 2, s1, s0);
         }
         if (t + 2 == n_tiles) {
-          step(Yes{}, t, t + 1, s0, s1);
-          step(No{}, t + 1, 0, s1, s0);
+          step(Yes{}, t, valid_of(t), t + 1, s0, s1);
+          step(No{}, t + 1, valid_of(t + 1), 0, s1, s0);
         } else {
-          step(No{}, t, 0, s0, s1);
+          step(No{}, t, valid_of(t), 0, s0, s1);
         }
       }
       finish(r0);
@@ -430,7 +451,7 @@ __global__ __launch_bounds__(64 * NW) void k_cross_attn(CrossParams p) {
         if (t + 1 < n_tiles) fetch(t_begin + t + 1, x);
         floatx16 sc[2], none[2];
         scores(t & 1, sc);
-        step(No{}, t & 1, 0, sc, none);
+        step(No{}, t & 1, valid_of(t & 1), 0, sc, none);
         if (t + 1 < n_tiles) put((t + 1) & 1, x);
         __syncthreads();
       }
@@ -457,12 +478,16 @@ __global__ __launch_bounds__(256) void k_cross_join(CrossParams p) {
   const float l = wave_sum(ml.y * weight), inv = l == 0.f ? 0.f : 1.f / l;
   const int c = std::min(2 * lane, p.dh - 2);
   float2 a = make_float2(0.f, 0.f);
-
-  for (int z = 0; z < p.parts; ++z) {
-    const float w = __uint_as_float((unsigned)__builtin_amdgcn_readlane((int)__float_as_uint(weight), z));
-    const float2 v = *reinterpret_cast<const float2 *>(p.part_o + (at + z * step) * p.dh + c);
-    a.x += w == 0.f ? 0.f : v.x * w;
-    a.y += w == 0.f ? 0.f : v.y * w;
+  for (int z0 = 0; z0 < p.parts; z0 += 8) {
+    float2 v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = *reinterpret_cast<const float2 *>(p.part_o + (at + std::min(z0 + j, p.parts - 1) * step) * p.dh + c);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {   // lanes past the parts have no weight
+      const float w = __uint_as_float((unsigned)__builtin_amdgcn_readlane((int)__float_as_uint(weight), z0 + j));
+      a.x += w == 0.f ? 0.f : v[j].x * w;
+      a.y += w == 0.f ? 0.f : v[j].y * w;
+    }
   }
   if (2 * lane < p.dh) {
     bf16x2 v;
@@ -487,7 +512,7 @@ int launch_as(const CrossParams &p, hipStream_t s) {
 template <int KS>
 int launch_form(int waves, const CrossParams &p, hipStream_t s) {
   constexpr int ST = KS == 8 ? 4 : 5;   // as many stages as the LDS holds
-  if (waves == 1) return p.parts > 1 ? launch_as<KS, 1, 2, true>(p, s) : launch_as<KS, 1, 2, false>(p, s);
+  if (waves == 1) return p.parts > 1 ? launch_as<KS, 1, 1, true>(p, s) : launch_as<KS, 1, 1, false>(p, s);
   return p.parts > 1 ? launch_as<KS, 8, ST, true>(p, s) : launch_as<KS, 8, ST, false>(p, s);
 }
 

@@ -143,14 +143,15 @@ __device__ __forceinline__ floatx16 mfma_mx4(intx4 a, int sa, intx4 b, int sb, f
   return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(A, B, c, 4, 4, SEL, sa, SEL, sb);
 }
 
-template <int BM_, int BN_, int WGM_, int WGN_, int NS_, int PER_CU_>
+template <int BM_, int BN_, int WGM_, int WGN_, int NS_, int PER_CU_, int PK_ = 1>
 struct Mx4Cfg {
   static constexpr int BM = BM_, BN = BN_, WGM = WGM_, WGN = WGN_, NS = NS_, PER_CU = PER_CU_;
+  static constexpr int PK = PK_;                             // panels of a stage
   static constexpr int NW = WGM * WGN, TM = BM / (32 * WGM), TN = BN / (32 * WGN);
   static constexpr int SC = (BM + BN) * 64;                  // scales behind the codes
-  static constexpr int STAGE = (BM + BN) * 68;
+  static constexpr int PANEL = (BM + BN) * 68, STAGE = PK * PANEL;
   static constexpr int NC = (BM + BN) / 16, NSC = (BM + BN) / 64;   // wave-wide loads of codes (16 rows) and scales (64 rows)
-  static constexpr int CJ = (NC + NW - 1) / NW, SJ = (NSC + NW - 1) / NW, NJ = CJ + SJ;
+  static constexpr int CJ = (NC + NW - 1) / NW, SJ = (NSC + NW - 1) / NW, NJ = PK * (CJ + SJ);
   static constexpr int PITCH_B = TN * 64 + 16, PITCH_F = 32 * 4 + 16;   // staged rows of the epilogues
   static constexpr int EPI_WAVE = 32 * (PITCH_B > PITCH_F ? PITCH_B : PITCH_F);
   static constexpr int SMEM = NS * STAGE + NW * EPI_WAVE;
@@ -215,23 +216,27 @@ __global__ __launch_bounds__(64 * C::NW, C::NW * C::PER_CU / 4) void k_mx4_gemm(
     const __amdgpu_buffer_rsrc_t r_wc = __builtin_amdgcn_make_buffer_rsrc((void *)p.wc, 0, -1, 0x00020000);
     const __amdgpu_buffer_rsrc_t r_us = __builtin_amdgcn_make_buffer_rsrc((void *)p.us, 0, -1, 0x00020000);
     const __amdgpu_buffer_rsrc_t r_ws = __builtin_amdgcn_make_buffer_rsrc((void *)p.ws, 0, -1, 0x00020000);
-    const unsigned pc_u = (unsigned)ld_panel * (unsigned)p.N * 64u, pc_w = (unsigned)ld_panel * (unsigned)p.n * 64u;
-    unsigned char *const at = smem + ld_st * C::STAGE;
 #pragma unroll
-    for (int j = 0; j < C::CJ; ++j) {
-      const int i = std::min(wave + NW * j, C::NC - 1);
-      if (i * 16 < BM) MX4_LOAD_TO_LDS(r_uc, (lds_ptr_t)(at + i * 1024), 16, vc[j], pc_u, 0, 0);
-      else MX4_LOAD_TO_LDS(r_wc, (lds_ptr_t)(at + i * 1024), 16, vc[j], pc_w, 0, 0);
-    }
+    for (int sub = 0; sub < C::PK; ++sub) {
+      const unsigned from = C::PK == 1 ? ld_panel : std::min(ld_panel + sub, p.panels - 1);
+      const unsigned pc_u = from * (unsigned)p.N * 64u, pc_w = from * (unsigned)p.n * 64u;
+      unsigned char *const at = smem + ld_st * C::STAGE + sub * C::PANEL;
 #pragma unroll
-    for (int j = 0; j < C::SJ; ++j) {
-      const int i = std::min(wave + NW * j, C::NSC - 1);
-      if (i * 64 < BM) MX4_LOAD_TO_LDS(r_us, (lds_ptr_t)(at + C::SC + i * 256), 4, vs[j], pc_u >> 4, 0, 0);
-      else MX4_LOAD_TO_LDS(r_ws, (lds_ptr_t)(at + C::SC + i * 256), 4, vs[j], pc_w >> 4, 0, 0);
+      for (int j = 0; j < C::CJ; ++j) {
+        const int i = std::min(wave + NW * j, C::NC - 1);
+        if (i * 16 < BM) MX4_LOAD_TO_LDS(r_uc, (lds_ptr_t)(at + i * 1024), 16, vc[j], pc_u, 0, 0);
+        else MX4_LOAD_TO_LDS(r_wc, (lds_ptr_t)(at + i * 1024), 16, vc[j], pc_w, 0, 0);
+      }
+#pragma unroll
+      for (int j = 0; j < C::SJ; ++j) {
+        const int i = std::min(wave + NW * j, C::NSC - 1);
+        if (i * 64 < BM) MX4_LOAD_TO_LDS(r_us, (lds_ptr_t)(at + C::SC + i * 256), 4, vs[j], pc_u >> 4, 0, 0);
+        else MX4_LOAD_TO_LDS(r_ws, (lds_ptr_t)(at + C::SC + i * 256), 4, vs[j], pc_w >> 4, 0, 0);
+      }
     }
     ld_st = ld_st + 1 == NS ? 0 : ld_st + 1;
-    if (ld_panel + 1 < p.panels) {
-      ++ld_panel;
+    if (ld_panel + C::PK < p.panels) {
+      ld_panel += C::PK;
     } else {
       int tm, tn;
       if (tile_of(p, ld_round + 1, tm, tn)) {
@@ -272,12 +277,7 @@ __global__ __launch_bounds__(64 * C::NW, C::NW * C::PER_CU / 4) void k_mx4_gemm(
       for (int b = 0; b < TM; ++b)
 #pragma unroll
         for (int e = 0; e < 16; ++e) acc[a][b][e] = (float)bias[a][e >> 2][e & 3];
-    for (int panel = 0; panel < p.panels; ++panel) {
-      if (round > 0 && panel < NS - 1) wait_vmcnt<C::AHEAD_FIRST>();
-      else wait_vmcnt<C::AHEAD>();
-      lds_barrier();   // this panel is complete, and everybody is done with the one before, whose stage is filled next
-      issue();
-      const unsigned char *const at = smem + st * C::STAGE;
+    auto multiply = [&](const unsigned char *at) {
       int su[TM], sw[TN];
       intx4 uf[2][TM], wf[2][TN];
 #pragma unroll
@@ -304,6 +304,19 @@ __global__ __launch_bounds__(64 * C::NW, C::NW * C::PER_CU / 4) void k_mx4_gemm(
       for (int a = 0; a < TN; ++a)
 #pragma unroll
         for (int b = 0; b < TM; ++b) acc[a][b] = mfma_mx4<2>(wf[1][a], sw[a], uf[1][b], su[b], acc[a][b]);
+    };
+    for (int panel = 0, step = 0; panel < p.panels; panel += C::PK, ++step) {
+      if (round > 0 && step < NS - 1) wait_vmcnt<C::AHEAD_FIRST>();
+      else wait_vmcnt<C::AHEAD>();
+      lds_barrier();   // this stage is complete, and everybody is done with the one before, which is filled next
+      issue();
+      const unsigned char *const at = smem + st * C::STAGE;
+      if (C::PK == 1 || panel + C::PK <= p.panels) {
+#pragma unroll
+        for (int sub = 0; sub < C::PK; ++sub) multiply(at + sub * C::PANEL);
+      } else {
+        for (int sub = 0; panel + sub < p.panels; ++sub) multiply(at + sub * C::PANEL);
+      }
       st = st + 1 == NS ? 0 : st + 1;
     }
 
@@ -588,10 +601,11 @@ int launch_mx4_gemm(int epilogue, const Mx4GemmArgs &a, hipStream_t s) {
   // Tiles of 128 x 128, three workgroups a CU, as soon as every CU has one: their epilogues run under the others' products.  The residual
   // update holds rows of the stream too and takes two a CU, and from two rounds of the chip on 256 x 256, which draws fewer operands
   // through the L2.  us, 64 x 64 / 128 x 128 / 256 x 256: 2304 x 4608 x 1152 20.5 / 13.8 / 17.0, 48600 x 4608 x 1152 with GELU 340 / 205 / 246;
-  // residual 2304 x 1152 x 4608 20.9 / 22.7 / 40.4, 12960 87 / 59 / 62, 48600 366 / 262 / 247.
+  // residual 2304 x 1152 x 4608 20.9 / 22.7 / 40.4, 12960 87 / 59 / 62, 48600 366 / 262 / 247.  With two panels between barriers the small tile
+  // takes 20.3 and, 300 x 1152 x 4608, 10.4 in place of 12.3.
   const int64_t t128 = ((a.N + 127) / 128) * ((a.n + 127) / 128), t256 = ((a.N + 255) / 256) * ((a.n + 255) / 256);
   const int64_t cus = device_cus();
-  if (t128 < cus) return launch_tile<Mx4Cfg<64, 64, 2, 2, 4, 3>>(epilogue, p, s);
+  if (t128 < cus) return launch_tile<Mx4Cfg<64, 64, 2, 2, 2, 3, 2>>(epilogue, p, s);
   if (epilogue != 2) return launch_tile<Mx4Cfg<128, 128, 2, 2, 2, 3>, false, true>(epilogue, p, s);
   if (t256 < 2 * cus) return launch_tile<Mx4Cfg<128, 128, 2, 2, 3, 2>, true, false>(epilogue, p, s);
   return launch_tile<Mx4Cfg<256, 256, 2, 4, 3, 1>, true, false>(epilogue, p, s);
