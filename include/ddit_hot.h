@@ -300,7 +300,8 @@ int ddit_mx4_dequantize(const void *codes, const void *scales, int64_t rows, int
 /* ddit_linear_fwd with both operands in mx4: out = Q(u) W^T + bias with the epilogues of ddit_linear_fwd, fp32 sums, except that the
  * residual update reads resid and writes resid_out (fp32 [N,n]; they may be the same).  W_codes, W_scales: the weight [n,k] as
  * ddit_mx4_quantize lays it out; bias bf16 [n] or NULL.  ddit_linear_mx4_fwd takes u bf16 [N,k] and quantises it on the way, in
- * a workspace (256-byte aligned, ddit_linear_mx4_workspace_bytes(); free again when the call's work is done);
+ * a workspace (256-byte aligned, ddit_linear_mx4_workspace_bytes(); free again when the call's work is done: calls that overlap in time
+ * need one each);
  * ddit_linear_mx4_codes_fwd takes it quantised already, as by several linears that share u.  No output may overlap an input but
  * resid_out resid.  n below 2^24, ld_out below 2^25.  N = 0 as above. */
 int ddit_linear_mx4_workspace_bytes(int64_t N, int32_t n, int32_t k, size_t *bytes_out);
@@ -324,7 +325,7 @@ int ddit_linear_mx4_codes_fwd(int epilogue, const void *u_codes, const void *u_s
  * q, o bf16 [q_rows, H, dh], k, v bf16 [kv_rows, H_kv, dh], rows ld_* elements apart (slices of wider buffers as in ddit_attn_fwd);
  * query head h reads key head h / (H / H_kv).  dh: a multiple of 8, at most 128.  scale > 0.  lse_or_null fp32 [q_rows, H].
  * o may not overlap an input.  workspace: ddit_cross_attn_packed_workspace_bytes() bytes, 256-byte aligned (NULL if 0), free again when the
- * call's work is done; the bytes depend on the totals alone.  q_rows * H up to 2^30, leading
+ * call's work is done (calls that overlap in time need one each); the bytes depend on the totals alone.  q_rows * H up to 2^30, leading
  * dimensions below 2^22.  q_rows = 0: arguments are validated, nothing is enqueued. */
 int ddit_cross_attn_packed_workspace_bytes(int32_t B, int64_t q_rows, int64_t kv_rows, int32_t H, int32_t dh, size_t *bytes_out);
 int ddit_cross_attn_packed_fwd(const void *q, int64_t ld_q, const int32_t *q_offsets, const void *k, const void *v, int64_t ld_kv,

@@ -153,7 +153,8 @@ __global__ __launch_bounds__(64 * NW) void k_cross_attn(CrossParams p) {
     const int i = tid + 64 * NW * j, row = i / C::CH, c = i - row * C::CH;
     piece_at[j] = row < KT && c < pieces ? ((unsigned)row * (unsigned)p.ld_kv + c * 8) * 2u : NOWHERE;
   }
-  const unsigned frag_at = ((unsigned)l32 * (unsigned)p.ld_kv + 8 * lh) * 2u;
+  // (the whole offset is the lane's own: whether a scalar one counts where a buffer's end is checked is described both ways)
+  const unsigned frag_at[2] = {((unsigned)l32 * (unsigned)p.ld_kv + 8 * lh) * 2u, ((unsigned)(32 + l32) * (unsigned)p.ld_kv + 8 * lh) * 2u};
   auto fetch = [&](int tile, Pieces &x) {
     const int left = std::min(n_keys - tile * KT, KT);
     const int64_t bytes = ((int64_t)(left - 1) * p.ld_kv + p.dh) * 2, at = (int64_t)tile * KT * p.ld_kv;
@@ -161,7 +162,7 @@ __global__ __launch_bounds__(64 * NW) void k_cross_attn(CrossParams p) {
     if constexpr (ALONE) {
 #pragma unroll
       for (int q = 0; q < NQ; ++q)   // key 32 (q % 2) + l32, k-step q / 2
-        x.k[q] = __builtin_amdgcn_raw_buffer_load_b128(ksrc, 2 * (q >> 1) + lh < pieces ? frag_at + (q >> 1) * 32 : NOWHERE, (q & 1) * 64 * (int)p.ld_kv, 0);
+        x.k[q] = __builtin_amdgcn_raw_buffer_load_b128(ksrc, 2 * (q >> 1) + lh < pieces ? frag_at[q & 1] + (q >> 1) * 32 : NOWHERE, 0, 0);
     }
 #pragma unroll
     for (int j = 0; j < CJ; ++j) {
@@ -524,11 +525,13 @@ int waves_for(int B, int64_t rows) { return rows <= (int64_t)64 * B ? 1 : 8; }
 namespace ddit {
 
 // From the totals alone, since the lengths are on the device, and for the whole chip whatever device is current, since the answer sizes workspaces:
-// parts of 128 keys and more, as many as make one round of the chip (a workgroup of eight wavefronts fills a CU, four of one do).
+// parts of 128 keys and more, as many as make one round of the chip (a workgroup of eight wavefronts fills a CU, four of one do).  Not for
+// fewer than 1024 states in all, where the second launch takes longer than what it saves (22 queries, 485 states: 10.9 us in 3 parts).
 int cross_attn_parts(int B, int64_t q_rows, int64_t kv_rows, int H, int H_kv) {
   const int64_t rows = q_rows * (H / H_kv);
   const int waves = waves_for(B, rows);
   const int64_t units = (rows / (32 * waves) + B) * H_kv;
+  if (kv_rows < 1024) return 1;
   return (int)std::max<int64_t>(1, std::min<int64_t>({(int64_t)32, (waves == 1 ? 1024 : 256) / units, kv_rows / 128}));
 }
 
