@@ -19,7 +19,6 @@
 #include "ddit_common.hpp"
 
 #include <algorithm>
-#include <type_traits>
 
 namespace {
 
@@ -128,7 +127,7 @@ __global__ __launch_bounds__(64 * NW) void k_cross_attn(CrossParams p) {
   auto buffer = [](const void *at, int64_t bytes) {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(at), 0, (int)std::min<int64_t>(bytes, 0x7fffffff), 0x00020000);
   };
-  constexpr bool Q_AHEAD = NW > 1 && KS <= 6;   // (with wider heads the registers are full)
+  constexpr bool Q_AHEAD = NW == 8 && KS <= 6;   // (with wider heads, or three wavefronts a SIMD, the registers are full)
   bf16x8 qf[KS], qn[Q_AHEAD ? KS : 1];
   auto fetch_q = [&](int r0, bf16x8 (&to)[KS]) {   // rows past the end: the last one again
     const int r = std::min(r0 + l32, slot.end - 1), q0 = std::min(r0, slot.end - 1) / p.group, q = r / p.group;
@@ -217,22 +216,11 @@ __global__ __launch_bounds__(64 * NW) void k_cross_attn(CrossParams p) {
 #pragma unroll
     for (int q = 0; q < NQ; ++q) s[q & 1] = mfma32(k_frag(st, q), qf[q >> 1], s[q & 1]);
   };
-#define XA_FENCE() __builtin_amdgcn_sched_barrier(0)
-  // One tile: softmax of its scores and O^T += V^T P^T, with the next tile's scores formed on the way.  A wavefront issues in order, so the
-  // matrix instructions are threaded by hand through the vector arithmetic, which takes longer than they do: one after every two
-  // exponentials, the next tile's scores first, then those of O whose 16 keys' weights are there.  K fragments are read four instructions
-  // ahead, V fragments a chunk of 16 keys ahead.
-  auto step = [&](auto next_tag, int st, uint64_t bits, int st_next, floatx16 (&s)[2], floatx16 (&s_next)[2]) {
-    constexpr bool NEXT = decltype(next_tag)::value;
-    constexpr int KD = 4, NS = NEXT ? NQ : 0, M = NS + NPV;
-    bf16x8 kf[KD];
-    if constexpr (NEXT) {
-#pragma unroll
-      for (int q = 0; q < KD; ++q) kf[q] = k_frag(st_next, q);
-    }
-    floatx16 zero;
-#pragma unroll
-    for (int e = 0; e < 16; ++e) zero[e] = 0.f;
+  // One tile: softmax of its scores and O^T += V^T P^T.  A wavefront issues in order, so the matrix instructions are threaded by hand through
+  // the vector arithmetic, which takes longer than they do: one after every two exponentials, as soon as its 16 keys' weights are there.  V
+  // fragments are read a chunk of 16 keys ahead.  (The next tile's scores in between as well, and room for them, changed nothing for 64 to 80
+  // features and spilled registers above: 2 x 48600 x 256 of 96 228 / 206 us, of 128 322 / 235.)
+  auto step = [&](int st, uint64_t bits, floatx16 (&s)[2]) {
     const unsigned valid[2] = {(unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)bits), (unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)(bits >> 32))};
     if ((valid[0] & valid[1]) != ~0u) {
 #pragma unroll
@@ -245,25 +233,11 @@ __global__ __launch_bounds__(64 * NW) void k_cross_attn(CrossParams p) {
         }
       }
     }
-    XA_FENCE();
-#define XA_SLOT_QK(Q)                                                       \
-  do {                                                                      \
-    s_next[(Q) & 1] = mfma32(kf[(Q) % KD], qf[(Q) >> 1], (Q) < 2 ? zero : s_next[(Q) & 1]);  \
-    if ((Q) + KD < NQ) kf[(Q) % KD] = k_frag(st_next, (Q) + KD);            \
-  } while (0)
-    int slot = 0;
-    if constexpr (NEXT) { XA_SLOT_QK(0); slot = 1; }
-    XA_FENCE();
     float mx = fmaxf(s[0][0], s[0][1]);
 #pragma unroll
     for (int e = 2; e < 16; ++e) mx = fmaxf(mx, s[0][e]);
-    XA_FENCE();
-    if constexpr (NEXT) { XA_SLOT_QK(1); slot = 2; }
-    XA_FENCE();
 #pragma unroll
     for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[1][e]);
-    XA_FENCE();
-    if constexpr (NEXT) { XA_SLOT_QK(2); slot = 3; }
     const Swapped both = swap_halves(__float_as_uint(mx), __float_as_uint(mx));
     mx = fmaxf(__uint_as_float(both.a), __uint_as_float(both.b));
     const bool move = mx > m_run + p.rebase;
@@ -287,9 +261,15 @@ __global__ __launch_bounds__(64 * NW) void k_cross_attn(CrossParams p) {
         vf[kc & 1][d] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
       }
     };
+    auto update = [&](int v) {   // the v-th of the tile's matrix instructions
+      const int kc = v / C::DT, d = v - kc * C::DT;
+      if (d == 0 && kc < 3) v_frags(kc + 1);
+      o[d] = mfma32(vf[kc & 1][d], pf[kc], o[d]);
+    };
     v_frags(0);
-    XA_FENCE();
+    __builtin_amdgcn_sched_barrier(0);
     float sum = 0.f;
+    int v = 0;
 #pragma unroll
     for (int g = 0; g < 16; ++g) {
 #pragma unroll
@@ -298,36 +278,15 @@ __global__ __launch_bounds__(64 * NW) void k_cross_attn(CrossParams p) {
         sum += w;
         pf[e >> 3][e & 7] = (bf16_t)w;
       }
-      XA_FENCE();
-      if (slot < NS) {
-        if constexpr (NEXT) XA_SLOT_QK(slot);
-        ++slot;
-      } else if (slot < M) {
-        const int v = slot - NS, kc = v / C::DT, d = v - kc * C::DT;
-        if (g >= 4 * kc + 3) {
-          if (d == 0 && kc < 3) v_frags(kc + 1);
-          o[d] = mfma32(vf[kc & 1][d], pf[kc], o[d]);
-          ++slot;
-        }
-      }
-      XA_FENCE();
+      __builtin_amdgcn_sched_barrier(0);
+      if (g >= 4 * (v / C::DT) + 3) update(v++);
+      __builtin_amdgcn_sched_barrier(0);
     }
 #pragma unroll
-    for (int sl = 0; sl < M; ++sl)
-      if (sl >= slot) {
-        if (sl < NS) {
-          if constexpr (NEXT) XA_SLOT_QK(sl);
-        } else {
-          const int v = sl - NS, kc = v / C::DT, d = v - kc * C::DT;
-          if (d == 0 && kc < 3) v_frags(kc + 1);
-          o[d] = mfma32(vf[kc & 1][d], pf[kc], o[d]);
-        }
-      }
+    for (int w = 0; w < NPV; ++w)
+      if (w >= v) update(w);
     l_run += sum;
-#undef XA_SLOT_QK
   };
-  using Yes = std::true_type;
-  using No = std::false_type;
   auto finish = [&](int r0) {
     const int r = r0 + l32, q = r / p.group, h = h0 + r - q * p.group;
     const bool in = r < slot.end;
@@ -396,7 +355,7 @@ __global__ __launch_bounds__(64 * NW) void k_cross_attn(CrossParams p) {
     if (n_tiles > 0) fetch(t_begin, x);
     begin(r_first);
     for (int t = 0; t < n_tiles; ++t) {
-      floatx16 sc[2], none[2];
+      floatx16 sc[2];
 #pragma unroll
       for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
@@ -406,7 +365,7 @@ __global__ __launch_bounds__(64 * NW) void k_cross_attn(CrossParams p) {
       put(0, x);
       const uint64_t bits = x.bits;
       if (t + 1 < n_tiles) fetch(t_begin + t + 1, x);
-      step(No{}, 0, bits, 0, sc, none);
+      step(0, bits, sc);
     }
     finish(r_first);
   } else if (n_tiles <= ST) {
@@ -423,20 +382,10 @@ __global__ __launch_bounds__(64 * NW) void k_cross_attn(CrossParams p) {
     __syncthreads();
     for (int r0 = r_first; r0 < slot.end; r0 += QT) {
       begin(r0);
-      if (n_tiles > 0) {
-        floatx16 s0[2], s1[2];
-        scores(0, s0);
-        int t = 0;
-        for (; t + 2 < n_tiles; t += 2) {
-          step(Yes{}, t, valid_of(t), t + 1, s0, s1);
-          step(Yes{}, t + 1, valid_of(t + 1), t + 2, s1, s0);
-        }
-        if (t + 2 == n_tiles) {
-          step(Yes{}, t, valid_of(t), t + 1, s0, s1);
-          step(No{}, t + 1, valid_of(t + 1), 0, s1, s0);
-        } else {
-          step(No{}, t, valid_of(t), 0, s0, s1);
-        }
+      for (int t = 0; t < n_tiles; ++t) {
+        floatx16 sc[2];
+        scores(t, sc);
+        step(t, valid_of(t), sc);
       }
       finish(r0);
     }
@@ -450,9 +399,9 @@ __global__ __launch_bounds__(64 * NW) void k_cross_attn(CrossParams p) {
       __syncthreads();
       for (int t = 0; t < n_tiles; ++t) {
         if (t + 1 < n_tiles) fetch(t_begin + t + 1, x);
-        floatx16 sc[2], none[2];
+        floatx16 sc[2];
         scores(t & 1, sc);
-        step(No{}, t & 1, valid_of(t & 1), 0, sc, none);
+        step(t & 1, valid_of(t & 1), sc);
         if (t + 1 < n_tiles) put((t + 1) & 1, x);
         __syncthreads();
       }
@@ -514,11 +463,18 @@ template <int KS>
 int launch_form(int waves, const CrossParams &p, hipStream_t s) {
   constexpr int ST = KS == 8 ? 4 : 5;   // as many stages as the LDS holds
   if (waves == 1) return p.parts > 1 ? launch_as<KS, 1, 1, true>(p, s) : launch_as<KS, 1, 1, false>(p, s);
+  if constexpr (KS <= 6)
+    if (waves == 12) return launch_as<KS, 12, ST, false>(p, s);
   return p.parts > 1 ? launch_as<KS, 8, ST, true>(p, s) : launch_as<KS, 8, ST, false>(p, s);
 }
 
-// Wavefronts of a workgroup, for `rows` rows a key head: one where sequences have few, on average
-int waves_for(int B, int64_t rows) { return rows <= (int64_t)64 * B ? 1 : 8; }
+// Wavefronts of a workgroup, for `rows` rows a key head: one where sequences have few, on average; three a SIMD for heads whose registers allow it, from
+// two rounds of the chip on; else two.  us, 8 / 12, 16 heads of 72: 97200 rows x 300 states 245 / 233, 48600 x 1024 369 / 308, 2304 x 300 15.0 / 16.5; of 64
+// 97200 x 256 163 / 149; of 128 254 / 408.
+int waves_for(int B, int64_t rows, int H_kv, int dh) {
+  if (rows <= (int64_t)64 * B) return 1;
+  return dh <= 96 && rows * H_kv >= 512 * 256 ? 12 : 8;
+}
 
 }  // namespace
 
@@ -529,10 +485,10 @@ namespace ddit {
 // fewer than 1024 states in all, where the second launch takes longer than what it saves (22 queries, 485 states: 10.9 us in 3 parts).
 int cross_attn_parts(int B, int64_t q_rows, int64_t kv_rows, int H, int H_kv) {
   const int64_t rows = q_rows * (H / H_kv);
-  const int waves = waves_for(B, rows);
-  const int64_t units = (rows / (32 * waves) + B) * H_kv;
+  const bool lone = waves_for(B, rows, H_kv, 0) == 1;
+  const int64_t units = (rows / (lone ? 32 : 256) + B) * H_kv;
   if (kv_rows < 1024) return 1;
-  return (int)std::max<int64_t>(1, std::min<int64_t>({(int64_t)32, (waves == 1 ? 1024 : 256) / units, kv_rows / 128}));
+  return (int)std::max<int64_t>(1, std::min<int64_t>({(int64_t)32, (lone ? 1024 : 256) / units, kv_rows / 128}));
 }
 
 int launch_cross_attn(const CrossAttnArgs &a, hipStream_t s) {
@@ -547,13 +503,13 @@ int launch_cross_attn(const CrossAttnArgs &a, hipStream_t s) {
   p.part_o = a.scratch;
   p.part_ml = p.parts > 1 ? a.scratch + (int64_t)p.parts * a.q_rows * a.H * a.dh : nullptr;
   const int64_t rows = a.q_rows * p.group;
-  const int waves = waves_for(a.B, rows);
+  const int waves = p.parts > 1 ? std::min(8, waves_for(a.B, rows, a.H_kv, a.dh)) : waves_for(a.B, rows, a.H_kv, a.dh);
   p.run = 32 * waves;
-  if (waves == 8 && p.parts == 1) {
+  if (waves > 1 && p.parts == 1) {
     // row tiles a workgroup walks over: a round of the chip takes that many and about one more for its set-up; counted for sequences of one length
     int64_t best = 0, cost = INT64_MAX;
     for (int64_t m = 1; m <= 16; ++m) {
-      const int64_t blocks = a.B * ((rows + a.B * 256 * m - 1) / (a.B * 256 * m)) * a.H_kv, c = (blocks + device_cus() - 1) / device_cus() * (m + 1);
+      const int64_t run = a.B * p.run * m, blocks = a.B * ((rows + run - 1) / run) * a.H_kv, c = (blocks + device_cus() - 1) / device_cus() * (m + 1);
       if (c < cost) { cost = c; best = m; }
     }
     p.run *= (int)best;

@@ -252,3 +252,11 @@ def test_no_states_and_no_queries_at_all(m):
     off = torch.zeros(2, dtype=torch.int32, device="cuda")
     m.ddit_cross_attn_packed_fwd(q[:0], H * dh, off, kv, kv, 2 * H * dh, off, None, 1, 0, 20, H, H, dh, 0.1, o[:0], H * dh, lse[:0], None)
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("H,G,dh", [(16, 16, 72), (16, 16, 64), (32, 16, 96), (16, 16, 128)])
+def test_many_rows(m, H, G, dh):
+    """From 512 row tiles of 256 on heads of up to 96 features take three wavefronts a SIMD: resident and streamed keys, a ragged end."""
+    tokens = [5000, 301, 0, 3100] if G == H else [2500, 301, 0, 1600]
+    check(m, tokens, [300, 77, 5, 700], H, G, dh, seed=dh)
+    check(m, tokens, [64, 0, 9, 257], H, G, dh, masked=True, seed=dh + 1)
