@@ -132,7 +132,7 @@ __device__ __forceinline__ void wait_vmcnt() {
 #if defined(__HIP_DEVICE_COMPILE__)
 #define MX4_LOAD_TO_LDS(...) __builtin_amdgcn_raw_ptr_buffer_load_lds(__VA_ARGS__)
 #else
-#define MX4_LOAD_TO_LDS(r, at, size, lane_offset, offset, ...) ((void)(r), (void)(at), (void)(lane_offset), (void)(offset))
+#define MX4_LOAD_TO_LDS(r, at, size, lane_offset, ...) ((void)(r), (void)(at), (void)(lane_offset))
 #endif
 
 // v_mfma_scale_f32_32x32x64_f8f6f4 on 4-bit operands: lane l holds 32 consecutive k, one scaled block, of row l % 32: k half l / 32.
@@ -212,26 +212,26 @@ __global__ __launch_bounds__(64 * C::NW, C::NW * C::PER_CU / 4) void k_mx4_gemm(
     for (int j = 0; j < C::SJ; ++j) vs[j] = row_of(std::min(wave + NW * j, C::NSC - 1) * 64 + lane) * 4u;
   };
   auto issue = [&]() {
-    const __amdgpu_buffer_rsrc_t r_uc = __builtin_amdgcn_make_buffer_rsrc((void *)p.uc, 0, -1, 0x00020000);
-    const __amdgpu_buffer_rsrc_t r_wc = __builtin_amdgcn_make_buffer_rsrc((void *)p.wc, 0, -1, 0x00020000);
-    const __amdgpu_buffer_rsrc_t r_us = __builtin_amdgcn_make_buffer_rsrc((void *)p.us, 0, -1, 0x00020000);
-    const __amdgpu_buffer_rsrc_t r_ws = __builtin_amdgcn_make_buffer_rsrc((void *)p.ws, 0, -1, 0x00020000);
+    // (the panel is in the buffers' bases: loads to LDS take no scalar offset here)
 #pragma unroll
     for (int sub = 0; sub < C::PK; ++sub) {
-      const unsigned from = C::PK == 1 ? ld_panel : std::min(ld_panel + sub, p.panels - 1);
-      const unsigned pc_u = from * (unsigned)p.N * 64u, pc_w = from * (unsigned)p.n * 64u;
+      const int64_t from = C::PK == 1 ? ld_panel : std::min(ld_panel + sub, p.panels - 1);
+      const __amdgpu_buffer_rsrc_t r_uc = __builtin_amdgcn_make_buffer_rsrc((void *)(p.uc + from * p.N * 64), 0, -1, 0x00020000);
+      const __amdgpu_buffer_rsrc_t r_wc = __builtin_amdgcn_make_buffer_rsrc((void *)(p.wc + from * p.n * 64), 0, -1, 0x00020000);
+      const __amdgpu_buffer_rsrc_t r_us = __builtin_amdgcn_make_buffer_rsrc((void *)(p.us + from * p.N * 4), 0, -1, 0x00020000);
+      const __amdgpu_buffer_rsrc_t r_ws = __builtin_amdgcn_make_buffer_rsrc((void *)(p.ws + from * p.n * 4), 0, -1, 0x00020000);
       unsigned char *const at = smem + ld_st * C::STAGE + sub * C::PANEL;
 #pragma unroll
       for (int j = 0; j < C::CJ; ++j) {
         const int i = std::min(wave + NW * j, C::NC - 1);
-        if (i * 16 < BM) MX4_LOAD_TO_LDS(r_uc, (lds_ptr_t)(at + i * 1024), 16, vc[j], pc_u, 0, 0);
-        else MX4_LOAD_TO_LDS(r_wc, (lds_ptr_t)(at + i * 1024), 16, vc[j], pc_w, 0, 0);
+        if (i * 16 < BM) MX4_LOAD_TO_LDS(r_uc, (lds_ptr_t)(at + i * 1024), 16, vc[j], 0, 0, 0);
+        else MX4_LOAD_TO_LDS(r_wc, (lds_ptr_t)(at + i * 1024), 16, vc[j], 0, 0, 0);
       }
 #pragma unroll
       for (int j = 0; j < C::SJ; ++j) {
         const int i = std::min(wave + NW * j, C::NSC - 1);
-        if (i * 64 < BM) MX4_LOAD_TO_LDS(r_us, (lds_ptr_t)(at + C::SC + i * 256), 4, vs[j], pc_u >> 4, 0, 0);
-        else MX4_LOAD_TO_LDS(r_ws, (lds_ptr_t)(at + C::SC + i * 256), 4, vs[j], pc_w >> 4, 0, 0);
+        if (i * 64 < BM) MX4_LOAD_TO_LDS(r_us, (lds_ptr_t)(at + C::SC + i * 256), 4, vs[j], 0, 0, 0);
+        else MX4_LOAD_TO_LDS(r_ws, (lds_ptr_t)(at + C::SC + i * 256), 4, vs[j], 0, 0, 0);
       }
     }
     ld_st = ld_st + 1 == NS ? 0 : ld_st + 1;
