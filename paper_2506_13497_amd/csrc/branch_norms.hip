@@ -8,7 +8,9 @@
 // stores; the next row of the same wavefront is on its way meanwhile.  What is common to a sample's rows - gate * g_post,
 // g_pre * (1 + scale), shift: up to eight vectors to read for three to keep - is formed once per workgroup and kept in LDS,
 // so workgroups take runs of consecutive rows, cut where the sample changes.
-// One wavefront a row up to 2048 features; four share a row above, and below where rows are few (see launch_norms).
+// One wavefront a row up to 2048 features; four share a row above, and below where rows are fewer than four a CU.
+// Measured: 48600 x 1152 139 us, 4.8 TB/s (a plain copy of that size 4.7), 12960 x 1152 40 us (29 with its operands in the memory-side
+// cache), 256 x 256 4.8 us.
 #include "ddit_common.hpp"
 
 #include <algorithm>

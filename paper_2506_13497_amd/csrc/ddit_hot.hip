@@ -1044,7 +1044,7 @@ int ddit_cross_attn_packed_fwd(const void *q, int64_t ld_q, const int32_t *q_off
     set_error("q, k, v, o, q_offsets and kv_offsets must not be NULL"); return DDIT_ERR_INVALID_ARG;
   }
   if (H_kv < 1 || H % H_kv) { set_error("H=%d query heads do not share H_kv=%d key heads evenly", H, H_kv); return DDIT_ERR_INVALID_ARG; }
-  if (!(scale > 0.f) || !(scale - scale == 0.f)) { set_error("scale=%g must be positive and finite", (double)scale); return DDIT_ERR_INVALID_ARG; }
+  if (!(scale > 0.f) || !(scale < 1e38f)) { set_error("scale=%g must be positive and finite", (double)scale); return DDIT_ERR_INVALID_ARG; }
   if (ld_q < (int64_t)H * dh || ld_kv < (int64_t)H_kv * dh || ld_o < (int64_t)H * dh) {
     set_error("leading dimensions (%lld,%lld,%lld) must be at least H*dh=%lld, H_kv*dh=%lld, H*dh", (long long)ld_q, (long long)ld_kv, (long long)ld_o,
               (long long)H * dh, (long long)H_kv * dh);

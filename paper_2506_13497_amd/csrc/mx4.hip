@@ -185,6 +185,11 @@ __device__ __forceinline__ bool tile_of(const Mx4Params &p, int round, int &tile
 // direct global -> LDS loads NS - 1 panels ahead; the stream of panels runs on into the workgroup's next tile, whose first panels
 // thus arrive ahead of the stores of this one.  A row's four 16-byte pieces are stored in the order piece ^ (row / 4 % 4), which spreads
 // the 16 rows that an LDS read serves at a time over all banks; the loads fetch them from there.
+// Bound: 48600 x 4608 x 1152 (205-228 us, 2.3-2.5 PFLOP/s; bf16 out 175-190) spends 85-97 us of it in matrix instructions alone, at the 1.8-2.0
+// GHz that the power limit leaves, 20 in LDS reads, 25 in loads, 30 to 55 in the epilogue's arithmetic and stores (each measured by leaving
+// the others out).  Rows leave through LDS in pieces of 128 bytes: whole lines.  Straight from the registers, after lane exchanges,
+// in pieces of 64 bytes, they took 213 us with GELU, 219 without and 290 to 350 in place of 250 in the residual update.  Reading the next
+// step's fragments under the products of this one: 0 to 6 % longer.
 template <class C, int EPI>
 __global__ __launch_bounds__(64 * C::NW, C::NW * C::PER_CU / 4) void k_mx4_gemm(Mx4Params p) {
   constexpr int BM = C::BM, BN = C::BN, NW = C::NW, TM = C::TM, TN = C::TN, NS = C::NS;
@@ -553,6 +558,7 @@ template <class C, bool RESIDUAL = true, bool DENSE = true>
 int launch_tile(int epi, Mx4Params p, hipStream_t s) {
   p.tiles_m = (int)((p.N + C::BM - 1) / C::BM);
   p.tiles_n = (p.n + C::BN - 1) / C::BN;
+  if ((int64_t)p.tiles_m * p.tiles_n > 0x7fffffff - 8) { ddit::set_error("mx4 linear: too many output tiles"); return -2; }
   // feature tiles of a group: their codes stay in an XCD's L2 while the token panels pass
   p.group_w = std::max(1, std::min(p.tiles_n, (int)((2 << 20) / ((int64_t)C::BN * p.panels * 64))));
   const int total = p.tiles_m * p.tiles_n, grid = std::min((total + 7) / 8, std::max(1, ddit::device_cus() * C::PER_CU / 8)) * 8;

@@ -121,7 +121,7 @@ def test_rows_of_no_sequence_stay(m):
     check(m, [3, 2], [1500, 800], 2, 2, 72, first=5, masked=True)
 
 
-@pytest.mark.parametrize("gain,scale", [(30.0, None), (1.0, 5.0), (0.0, None), (1.0, 1e-6)])
+@pytest.mark.parametrize("gain,scale", [(30.0, None), (1.0, 5.0), (0.0, None), (1.0, 1e-6), (1.0, 1e-39)])
 def test_peaked_and_flat(m, gain, scale):
     for tokens, states in [([100, 30], [200, 333]), ([2, 3], [2000, 1500])]:
         check(m, tokens, states, 2, 2, 72, gain=gain, scale=scale, seed=7)

@@ -105,7 +105,7 @@ def test_cross_packed_refusals(m):
     assert call() == 0 and call(mask=P(0x7001), lse=P(0x8004)) == 0
     assert call(q=None, o=None) == 0 and call(kv_rows=0, k=None, v=None) == 0
     for bad in (dict(q_rows=3, q=None), dict(k=None), dict(v=None), dict(q_rows=3, o=None), dict(q_off=None), dict(kv_off=None), dict(B=0), dict(q_rows=-1), dict(kv_rows=-1), dict(H=0),
-                dict(G=0), dict(G=3), dict(dh=0), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")), dict(ld_q=248),
+                dict(G=0), dict(G=3), dict(dh=0), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")), dict(scale=2e38), dict(ld_q=248),
                 dict(ld_kv=120), dict(ld_o=248)):
         assert call(**bad) == -1, bad
     for bad in (dict(dh=60), dict(dh=136, ld_q=1024, ld_kv=1024, ld_o=1024), dict(B=1 << 20), dict(q_rows=1 << 31), dict(kv_rows=1 << 31), dict(H=1 << 17), dict(ld_o=1 << 22), dict(ld_q=1 << 22), dict(ld_kv=1 << 22)):
