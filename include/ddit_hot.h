@@ -323,7 +323,8 @@ int ddit_linear_mx4_codes_fwd(int epilogue, const void *u_codes, const void *u_s
  * touched.)  A sequence may have no query, no state, or none that is left by key_mask_or_null: device uint8 [kv_rows], 0 = the state takes no
  * part, whatever its values; such queries get o = 0 and lse = -inf.  Rows of o and lse that belong to no sequence stay as they are.
  * q, o bf16 [q_rows, H, dh], k, v bf16 [kv_rows, H_kv, dh], rows ld_* elements apart (slices of wider buffers as in ddit_attn_fwd);
- * query head h reads key head h / (H / H_kv).  dh: a multiple of 8, at most 128.  0 < scale < 1e38.  lse_or_null fp32 [q_rows, H].
+ * query head h reads key head h / (H / H_kv).  dh: a multiple of 8, at most 128.  0 < scale < 1e38; scale q k itself may leave fp32 (q k may
+ * not), which an lse then does too, as an infinity, and o does not.  lse_or_null fp32 [q_rows, H].
  * o may not overlap an input.  workspace: ddit_cross_attn_packed_workspace_bytes() bytes, 256-byte aligned (NULL if 0), free again when the
  * call's work is done (calls that overlap in time need one each); the bytes depend on the totals alone.  q_rows * H up to 2^30, leading
  * dimensions below 2^22.  q_rows = 0: arguments are validated, nothing is enqueued. */

@@ -254,7 +254,15 @@ __global__ __launch_bounds__(64 * NW) void k_cross_attn(CrossParams p) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[d][e] *= alpha;
     }
-    const float ref = m_run == -INFINITY ? 0.f : m_run * p.scale_log2;
+    // exp2(s c - m c) with one rounding less: fine while m c, rounded once for all scores, is off by at most 2^-13.  Further out the
+    // maximum comes off first, before the difference is scaled, or its rounding error would swamp the exponent, and m c leave fp32.
+    float ref = m_run == -INFINITY ? 0.f : m_run * p.scale_log2;
+    if (__ballot(__builtin_fabsf(ref) > 4096.f)) {
+      const float off = m_run == -INFINITY ? 0.f : m_run;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) { s[0][e] -= off; s[1][e] -= off; }
+      ref = 0.f;
+    }
     const unsigned char *const va = smem + st * C::STAGE + tr;
     bf16x8 pf[4], vf[2][C::DT];
     auto v_frags = [&](int kc) {
