@@ -327,7 +327,8 @@ int ddit_linear_mx4_codes_fwd(int epilogue, const void *u_codes, const void *u_s
  * not), which an lse then does too, as an infinity, and o does not.  lse_or_null fp32 [q_rows, H].
  * o may not overlap an input.  workspace: ddit_cross_attn_packed_workspace_bytes() bytes, 256-byte aligned (NULL if 0), free again when the
  * call's work is done (calls that overlap in time need one each); the bytes depend on the totals alone.  q_rows * H up to 2^30, leading
- * dimensions below 2^22.  q_rows = 0: arguments are validated, nothing is enqueued. */
+ * dimensions below 2^22; a launch that needs 2^32 work-items (tens of thousands of requests of more than a hundred key heads and millions
+ * of queries) is DDIT_ERR_UNSUPPORTED.  q_rows = 0: arguments are validated, nothing is enqueued. */
 int ddit_cross_attn_packed_workspace_bytes(int32_t B, int64_t q_rows, int64_t kv_rows, int32_t H, int32_t dh, size_t *bytes_out);
 int ddit_cross_attn_packed_fwd(const void *q, int64_t ld_q, const int32_t *q_offsets, const void *k, const void *v, int64_t ld_kv,
                                const int32_t *kv_offsets, const uint8_t *key_mask_or_null, int32_t B, int64_t q_rows, int64_t kv_rows,

@@ -461,13 +461,16 @@ __global__ __launch_bounds__(256) void k_cross_join(CrossParams p) {
 
 template <int KS, int NW, int ST, bool PARTS>
 int launch_as(const CrossParams &p, hipStream_t s) {
+  const unsigned slots = (unsigned)((int64_t)p.q_rows * p.group / p.run + p.B);
+  const int64_t blocks = (int64_t)((slots + 7) / 8 * 8) * (p.H / p.group) * p.parts;
+  if (blocks * 64 * NW > 0xffffffff) {   // a launch counts its work-items in 32 bits
+    ddit::set_error("packed cross-attention: %lld workgroups of %d threads: too many", (long long)blocks, 64 * NW);
+    return -2;
+  }
   constexpr int smem = CrossCfg<KS, ST>::SMEM;
   static std::atomic<uint64_t> allowed;
   const int rc = ddit::allow_dynamic_lds(reinterpret_cast<const void *>(&k_cross_attn<KS, NW, ST, PARTS>), smem, &allowed);
   if (rc != 0) return rc;
-  const unsigned slots = (unsigned)((int64_t)p.q_rows * p.group / p.run + p.B);
-  const int64_t blocks = (int64_t)((slots + 7) / 8 * 8) * (p.H / p.group) * p.parts;
-  if (blocks > 0x7fffffff) { ddit::set_error("packed cross-attention: too many workgroups"); return -2; }
   hipLaunchKernelGGL((k_cross_attn<KS, NW, ST, PARTS>), dim3((unsigned)blocks), dim3(64 * NW), smem, s, p);
   return ddit::hip_fail(hipGetLastError(), "packed cross-attention launch");
 }
