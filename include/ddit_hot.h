@@ -290,7 +290,7 @@ int ddit_branch_norms_fwd(int norm, const void *f, int64_t ld_f, const void *g_p
  * saturate at 6.  A block that holds an Inf or a NaN gets the byte 255 and is NaN as a whole.
  * Layout of rows x k values: P = ceil(k / 128) panels, behind one another; a panel is [rows, 64] bytes of codes (byte j of a row: value
  * 128 panel + 2 j in the low half, 128 panel + 2 j + 1 in the high half) and, in an array of its own, [rows, 4] scale bytes.  Values
- * past k are 0.  k is a multiple of 8; rows * P * 64 below 2^31.
+ * past k are 0.  k is a multiple of 8; rows * P * 64 below 2^31, and P below 2^24 for the two calls that convert.
  * ddit_mx4_bytes: sizes of the two arrays (host only; needs no GPU).  ddit_mx4_quantize: x bf16 [rows,k], row stride ld_x, into them.
  * ddit_mx4_dequantize: the values that they stand for, bf16 [rows,k] (exact), row stride ld_out. */
 int ddit_mx4_bytes(int64_t rows, int32_t k, size_t *code_bytes_out, size_t *scale_bytes_out);

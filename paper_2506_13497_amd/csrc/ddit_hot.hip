@@ -924,6 +924,9 @@ static int check_mx4_copy(const void *dense, int64_t ld, int64_t rows, int32_t k
   if (ld % 8 || !aligned16(dense) || !aligned16(codes) || !aligned16(scales)) {
     set_error("pointers must be 16-byte aligned and leading dimensions multiples of 8"); return DDIT_ERR_ALIGNMENT;
   }
+  if (rows > 0 && mx4_panels(k) >= 1 << 24) {   // 256 threads each: a launch counts its work-items in 32 bits
+    set_error("mx4: k=%d: 2^24 panels or more are not supported", k); return DDIT_ERR_UNSUPPORTED;
+  }
   return DDIT_OK;
 }
 

@@ -18,3 +18,13 @@ def test_packed_attention_with_more_workgroups_than_a_launch_holds(m):
         scale=0.125, o=P(0x6000), ld_o=1024, lse=None, ws=None, bytes=0, stream=None))
     assert call() == -2 and "workgroups" in m.ddit_last_error()
     assert call(dh=128, ld_q=16384, ld_kv=16384, ld_o=16384) == -2
+
+
+def test_one_row_of_all_panels(m):
+    """2^24 panels of one row: a workgroup of 256 threads each."""
+    lib = m.binding._lib
+    for fn, args in ((lib.ddit_mx4_quantize, dict(x=P(0x1000), ld=1 << 31, rows=1, k=(1 << 31) - 8, codes=P(0x2000), scales=P(0x3000), stream=None)),
+                     (lib.ddit_mx4_dequantize, dict(codes=P(0x2000), scales=P(0x3000), rows=1, k=(1 << 31) - 8, x=P(0x1000), ld=1 << 31, stream=None))):
+        call = _caller(fn, args)
+        assert call() == -2 and "panels" in m.ddit_last_error()
+        assert call(rows=0) == 0
