@@ -205,8 +205,16 @@ def _ptr(t: Optional[torch.Tensor]):
     return None if t is None else C.c_void_p(t.data_ptr())
 
 
-# The current stream's handle without the Stream object around it, whose making takes as long as a kernel launch (2.8 us of 3.1).
-_raw_stream, _device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+# The current stream's handle without the Stream object around it, whose making takes as long as a kernel launch (2.8 us of 3.1).  torch
+# promises neither call: without both of them, its public ones.
+try:
+    _raw_stream, _device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+except AttributeError:
+    def _raw_stream(device):
+        return torch.cuda.current_stream(device).cuda_stream
+
+    def _device():
+        return torch.cuda.current_device()
 
 
 def _stream():
