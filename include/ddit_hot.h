@@ -313,6 +313,9 @@ int ddit_linear_mx4_codes_fwd(int epilogue, const void *u_codes, const void *u_s
                               const void *bias, int64_t N, int32_t n, int32_t k, void *out, int64_t ld_out, const float *resid,
                               float *resid_out, const float *ada_table, const float *c6, int gate_row, int64_t tokens_per_sample,
                               void *hip_stream);
+/* Rows and columns of the output that a workgroup of these linears makes: 16 x 16 or 32 x 16 (few tokens: quantisation and product are one
+ * launch), or tiles of 64 x 64, 128 x 128 or 256 x 256.  compute_units as for ddit_linear_form.  Host only; needs no GPU. */
+int ddit_linear_mx4_form(int epilogue, int64_t N, int32_t n, int32_t k, int32_t compute_units, int32_t *rows_out, int32_t *cols_out);
 
 /* Cross-attention of requests packed one behind the other, each to its own encoder states (another length for each, as
  * the prompts of section 2.2's text condition have): for every b and head h, the queries in rows q_offsets[b] .. q_offsets[b+1]-1 of q attend
@@ -334,6 +337,11 @@ int ddit_cross_attn_packed_fwd(const void *q, int64_t ld_q, const int32_t *q_off
                                const int32_t *kv_offsets, const uint8_t *key_mask_or_null, int32_t B, int64_t q_rows, int64_t kv_rows,
                                int32_t H, int32_t H_kv, int32_t dh, float scale, void *o, int64_t ld_o, float *lse_or_null,
                                void *workspace, size_t workspace_bytes, void *hip_stream);
+/* The form that these totals take: wavefronts of a workgroup (1, 8 or 12), parts of the keys (1: no second launch), and the rows of a
+ * workgroup, a row being one query of one of the H / H_kv heads that share a key head.  compute_units as for ddit_linear_form.  Host only; needs
+ * no GPU. */
+int ddit_cross_attn_packed_form(int32_t B, int64_t q_rows, int64_t kv_rows, int32_t H, int32_t H_kv, int32_t dh, int32_t compute_units,
+                                int32_t *wavefronts_out, int32_t *parts_out, int32_t *rows_out);
 
 /* ---- output tiles of the linear: for tuning and for parity tests of every compiled tile ----
  * The linear is compiled for a short list of output tiles (rows x cols of out per workgroup), which callers can force, and for

@@ -35,7 +35,8 @@ EXPORTS = ["ddit_abi_version", "ddit_status_string", "ddit_last_error", "ddit_wo
            "ddit_buddy_create", "ddit_buddy_alloc", "ddit_buddy_release", "ddit_buddy_free_gpus", "ddit_buddy_destroy",
            "ddit_sched_simulate", "ddit_probe_mfma_bf16", "ddit_probe_stream_copy", "ddit_probe_stream_read", "ddit_probe_residual_stream",
            "ddit_branch_norms_fwd", "ddit_mx4_bytes", "ddit_mx4_quantize", "ddit_mx4_dequantize", "ddit_linear_mx4_workspace_bytes",
-           "ddit_linear_mx4_fwd", "ddit_linear_mx4_codes_fwd", "ddit_cross_attn_packed_workspace_bytes", "ddit_cross_attn_packed_fwd"]
+           "ddit_linear_mx4_fwd", "ddit_linear_mx4_codes_fwd", "ddit_linear_mx4_form", "ddit_cross_attn_packed_workspace_bytes",
+           "ddit_cross_attn_packed_fwd", "ddit_cross_attn_packed_form"]
 
 
 class ddit_shape(C.Structure):
@@ -185,6 +186,8 @@ def _load() -> C.CDLL:
     lib.ddit_linear_mx4_workspace_bytes.argtypes = [I64, I32, I32, C.POINTER(SZ)]
     lib.ddit_linear_mx4_fwd.argtypes = [C.c_int, VP, I64, VP, VP, VP, I64, I32, I32, VP, I64, VP, VP, VP, VP, C.c_int, I64, VP, SZ, VP]
     lib.ddit_linear_mx4_codes_fwd.argtypes = [C.c_int, VP, VP, VP, VP, VP, I64, I32, I32, VP, I64, VP, VP, VP, VP, C.c_int, I64, VP]
+    lib.ddit_linear_mx4_form.argtypes = [C.c_int, I64, I32, I32, I32] + [C.POINTER(I32)] * 2
+    lib.ddit_cross_attn_packed_form.argtypes = [I32, I64, I64, I32, I32, I32, I32] + [C.POINTER(I32)] * 3
     lib.ddit_cross_attn_packed_workspace_bytes.argtypes = [I32, I64, I64, I32, I32, C.POINTER(SZ)]
     lib.ddit_cross_attn_packed_fwd.argtypes = [VP, I64, VP, VP, VP, I64, VP, VP, I32, I64, I64, I32, I32, I32, C.c_float, VP, I64, VP, VP, SZ, VP]
     for n in EXPORTS:
@@ -610,6 +613,13 @@ def ddit_linear_mx4_codes_fwd(epilogue: int, u_codes, u_scales, W_codes, W_scale
     _check(_lib.ddit_linear_mx4_codes_fwd(epilogue, uc, us, wc, ws, pb, N, n, k, po, ld_out, px, pxo, pt, pc, gate_row, tokens_per_sample, stream))
 
 
+def ddit_linear_mx4_form(epilogue: int, N: int, n: int, k: int, compute_units: int = 0):
+    """-> (rows, columns) of a workgroup's output; 16 columns: the one launch of few tokens."""
+    v = [C.c_int32() for _ in range(2)]
+    _check(_lib.ddit_linear_mx4_form(epilogue, N, n, k, compute_units, *[C.byref(x) for x in v]))
+    return v[0].value, v[1].value
+
+
 def ddit_cross_attn_packed_workspace_bytes(B: int, q_rows: int, kv_rows: int, H: int, dh: int) -> int:
     b = C.c_size_t(0)
     _check(_lib.ddit_cross_attn_packed_workspace_bytes(B, q_rows, kv_rows, H, dh, C.byref(b)))
@@ -621,6 +631,13 @@ def ddit_cross_attn_packed_fwd(q, ld_q: int, q_offsets, k, v, ld_kv: int, kv_off
     pq, qo, pk, pv, ko, pm, po, pl, pw, stream = _on_device(q, q_offsets, k, v, kv_offsets, key_mask, o, lse, workspace)
     _check(_lib.ddit_cross_attn_packed_fwd(pq, ld_q, qo, pk, pv, ld_kv, ko, pm, B, q_rows, kv_rows, H, H_kv, dh, scale, po, ld_o, pl, pw,
                                            _nbytes(workspace), stream))
+
+
+def ddit_cross_attn_packed_form(B: int, q_rows: int, kv_rows: int, H: int, H_kv: int, dh: int, compute_units: int = 0):
+    """-> (wavefronts of a workgroup, parts of the keys, rows of a workgroup)."""
+    v = [C.c_int32() for _ in range(3)]
+    _check(_lib.ddit_cross_attn_packed_form(B, q_rows, kv_rows, H, H_kv, dh, compute_units, *[C.byref(x) for x in v]))
+    return v[0].value, v[1].value, v[2].value
 
 
 def ddit_probe_mfma_bf16(operands, sink, iters: int) -> float:

@@ -506,6 +506,25 @@ int cross_attn_parts(int B, int64_t q_rows, int64_t kv_rows, int H, int H_kv) {
   return (int)std::max<int64_t>(1, std::min<int64_t>({(int64_t)32, (lone ? 1024 : 256) / units, kv_rows / 128}));
 }
 
+CrossForm cross_attn_form(int B, int64_t q_rows, int64_t kv_rows, int H, int H_kv, int dh, int cus) {
+  const int64_t rows = q_rows * (H / H_kv);
+  CrossForm f;
+  f.parts = cross_attn_parts(B, q_rows, kv_rows, H, H_kv);
+  f.waves = waves_for(B, rows, H_kv, dh);
+  if (f.parts > 1) f.waves = std::min(8, f.waves);
+  f.run = 32 * f.waves;
+  if (f.waves > 1 && f.parts == 1) {
+    // row tiles a workgroup walks over: a round of the chip takes that many and about one more for its set-up; counted for sequences of one length
+    int64_t best = 0, cost = INT64_MAX;
+    for (int64_t m = 1; m <= 16; ++m) {
+      const int64_t run = B * f.run * m, blocks = B * ((rows + run - 1) / run) * H_kv, c = (blocks + cus - 1) / cus * (m + 1);
+      if (c < cost) { cost = c; best = m; }
+    }
+    f.run *= (int)best;
+  }
+  return f;
+}
+
 int launch_cross_attn(const CrossAttnArgs &a, hipStream_t s) {
   if (a.q_rows == 0) return 0;
   CrossParams p;
@@ -514,25 +533,14 @@ int launch_cross_attn(const CrossAttnArgs &a, hipStream_t s) {
   p.B = a.B; p.q_rows = (int)a.q_rows; p.kv_rows = (int)a.kv_rows; p.H = a.H; p.group = a.H / a.H_kv; p.dh = a.dh;
   p.scale = a.scale; p.scale_log2 = a.scale * 1.4426950408889634f; p.rebase = std::min(8.f / p.scale_log2, 1e30f);
   p.o = reinterpret_cast<bf16_t *>(a.o); p.lse = a.lse;
-  p.parts = cross_attn_parts(a.B, a.q_rows, a.kv_rows, a.H, a.H_kv);
+  const CrossForm f = cross_attn_form(a.B, a.q_rows, a.kv_rows, a.H, a.H_kv, a.dh, device_cus());
+  p.parts = f.parts; p.run = f.run;
   p.part_o = a.scratch;
   p.part_ml = p.parts > 1 ? a.scratch + (int64_t)p.parts * a.q_rows * a.H * a.dh : nullptr;
-  const int64_t rows = a.q_rows * p.group;
-  const int waves = p.parts > 1 ? std::min(8, waves_for(a.B, rows, a.H_kv, a.dh)) : waves_for(a.B, rows, a.H_kv, a.dh);
-  p.run = 32 * waves;
-  if (waves > 1 && p.parts == 1) {
-    // row tiles a workgroup walks over: a round of the chip takes that many and about one more for its set-up; counted for sequences of one length
-    int64_t best = 0, cost = INT64_MAX;
-    for (int64_t m = 1; m <= 16; ++m) {
-      const int64_t run = a.B * p.run * m, blocks = a.B * ((rows + run - 1) / run) * a.H_kv, c = (blocks + device_cus() - 1) / device_cus() * (m + 1);
-      if (c < cost) { cost = c; best = m; }
-    }
-    p.run *= (int)best;
-  }
-  const int rc = p.dh <= 64 ? launch_form<4>(waves, p, s) : p.dh <= 80 ? launch_form<5>(waves, p, s) : p.dh <= 96 ? launch_form<6>(waves, p, s)
-                                                                                                              : launch_form<8>(waves, p, s);
+  const int rc = p.dh <= 64 ? launch_form<4>(f.waves, p, s) : p.dh <= 80 ? launch_form<5>(f.waves, p, s) : p.dh <= 96 ? launch_form<6>(f.waves, p, s)
+                                                                                                                  : launch_form<8>(f.waves, p, s);
   if (rc != 0 || p.parts == 1) return rc;
-  hipLaunchKernelGGL(k_cross_join, dim3((unsigned)(rows / 4 + p.B), (unsigned)a.H_kv), dim3(256), 0, s, p);
+  hipLaunchKernelGGL(k_cross_join, dim3((unsigned)(a.q_rows * p.group / 4 + p.B), (unsigned)a.H_kv), dim3(256), 0, s, p);
   return hip_fail(hipGetLastError(), "packed cross-attention join");
 }
 

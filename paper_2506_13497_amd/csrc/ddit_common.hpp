@@ -217,6 +217,8 @@ struct Mx4GemmArgs {
   int64_t tokens_per_sample;
 };
 bool mx4_one_launch(int64_t N, int n);   // whether a linear of N tokens and n features takes u as it is
+struct Mx4Form { int rows, cols; };      // output of a workgroup; 16 or 32 x 16: the launch that takes u as it is
+Mx4Form mx4_form(int epilogue, int64_t N, int n, int cus);
 int launch_mx4_gemm(int epilogue, const Mx4GemmArgs &a, hipStream_t s);
 
 // cross-attention of packed requests (cross_attn.hip)
@@ -229,6 +231,8 @@ struct CrossAttnArgs {
   float *scratch;                                   // cross_attn_parts() > 1: parts * q_rows * H * (dh + 2) floats
 };
 int cross_attn_parts(int B, int64_t q_rows, int64_t kv_rows, int H, int H_kv);   // in how many parts the keys are taken
+struct CrossForm { int waves, parts, run; };   // wavefronts of a workgroup, parts of the keys, rows (query, head of its group) a workgroup
+CrossForm cross_attn_form(int B, int64_t q_rows, int64_t kv_rows, int H, int H_kv, int dh, int cus);
 int launch_cross_attn(const CrossAttnArgs &a, hipStream_t s);
 
 // layers around the token-space step, solver

@@ -948,6 +948,17 @@ int ddit_linear_mx4_workspace_bytes(int64_t N, int32_t n, int32_t k, size_t *byt
   return DDIT_OK;
 }
 
+int ddit_linear_mx4_form(int epilogue, int64_t N, int32_t n, int32_t k, int32_t compute_units, int32_t *rows_out, int32_t *cols_out) {
+  if (epilogue < 0 || epilogue > 2) { set_error("unknown epilogue %d", epilogue); return DDIT_ERR_INVALID_ARG; }
+  DDIT_TRY(check_mx4(N, k, "N"));
+  if (n < 1) { set_error("linear: n=%d", n); return DDIT_ERR_INVALID_ARG; }
+  if (n % 8) { set_error("n=%d must be a multiple of 8", n); return DDIT_ERR_UNSUPPORTED; }
+  if (!rows_out || !cols_out) { set_error("rows_out and cols_out must not be NULL"); return DDIT_ERR_INVALID_ARG; }
+  const Mx4Form f = mx4_form(epilogue, N, n, compute_units > 0 ? compute_units : device_cus());
+  *rows_out = f.rows; *cols_out = f.cols;
+  return DDIT_OK;
+}
+
 // the arguments that the two linears share, into *g
 static int check_linear_mx4(int epilogue, const void *W_codes, const void *W_scales, const void *bias, int64_t N, int32_t n, int32_t k, void *out,
                             int64_t ld_out, const float *resid, float *resid_out, const float *ada_table, const float *c6, int gate_row,
@@ -1035,6 +1046,16 @@ int ddit_cross_attn_packed_workspace_bytes(int32_t B, int64_t q_rows, int64_t kv
   for (int g = 1; g * g <= H; ++g)
     if (H % g == 0) parts = std::max({parts, cross_attn_parts(B, q_rows, kv_rows, H, g), cross_attn_parts(B, q_rows, kv_rows, H, H / g)});
   *bytes_out = parts > 1 ? (size_t)parts * q_rows * H * (dh + 2) * 4 : 0;
+  return DDIT_OK;
+}
+
+int ddit_cross_attn_packed_form(int32_t B, int64_t q_rows, int64_t kv_rows, int32_t H, int32_t H_kv, int32_t dh, int32_t compute_units,
+                                int32_t *wavefronts_out, int32_t *parts_out, int32_t *rows_out) {
+  DDIT_TRY(check_cross_packed(B, q_rows, kv_rows, H, dh));
+  if (H_kv < 1 || H % H_kv) { set_error("H=%d query heads do not share H_kv=%d key heads evenly", H, H_kv); return DDIT_ERR_INVALID_ARG; }
+  if (!wavefronts_out || !parts_out || !rows_out) { set_error("wavefronts_out, parts_out and rows_out must not be NULL"); return DDIT_ERR_INVALID_ARG; }
+  const CrossForm f = cross_attn_form(B, q_rows, kv_rows, H, H_kv, dh, compute_units > 0 ? compute_units : device_cus());
+  *wavefronts_out = f.waves; *parts_out = f.parts; *rows_out = f.run;
   return DDIT_OK;
 }
 

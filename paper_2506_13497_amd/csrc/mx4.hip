@@ -591,6 +591,19 @@ int launch_mx4_dequantize(const void *codes, const void *scales, int64_t rows, i
 
 bool mx4_one_launch(int64_t N, int n) { return few_tokens(N, n); }
 
+Mx4Form mx4_form(int epilogue, int64_t N, int n, int cus) {
+  if (few_tokens(N, n)) return {N <= 16 ? 16 : 32, 16};
+  // Tiles of 128 x 128, three workgroups a CU, as soon as every CU has one: their epilogues run under the others' products.  The residual
+  // update holds rows of the stream too and takes two a CU, and from two rounds of the chip on 256 x 256, which draws fewer operands
+  // through the L2.  us, 64 x 64 / 128 x 128 / 256 x 256: 2304 x 4608 x 1152 20.5 / 13.8 / 17.0, 48600 x 4608 x 1152 with GELU 340 / 205 / 246;
+  // residual 2304 x 1152 x 4608 20.9 / 22.7 / 40.4, 12960 87 / 59 / 62, 48600 366 / 262 / 247.  With two panels between barriers the small tile
+  // takes 20.3 and, 300 x 1152 x 4608, 10.4 in place of 12.3.
+  const int64_t t128 = ((N + 127) / 128) * ((n + 127) / 128), t256 = ((N + 255) / 256) * ((n + 255) / 256);
+  if (t128 < cus) return {64, 64};
+  if (epilogue != 2 || t256 < 2 * cus) return {128, 128};
+  return {256, 256};
+}
+
 int launch_mx4_gemm(int epilogue, const Mx4GemmArgs &a, hipStream_t s) {
   if (a.N == 0) return 0;
   Mx4Params p;
@@ -600,21 +613,15 @@ int launch_mx4_gemm(int epilogue, const Mx4GemmArgs &a, hipStream_t s) {
   p.N = a.N; p.n = a.n; p.panels = (int)mx4_panels(a.k);
   p.out = reinterpret_cast<bf16_t *>(a.out); p.ld_out = a.ld_out; p.resid = a.resid; p.resid_out = a.resid_out;
   p.gate_tab = a.gate_tab; p.gate_c6 = a.gate_c6; p.gate_c6_stride = a.gate_c6_stride; p.tokens_per_sample = a.tokens_per_sample;
-  if (few_tokens(a.N, a.n)) {
+  const Mx4Form f = mx4_form(epilogue, a.N, a.n, device_cus());
+  if (f.cols == 16) {
     if (a.u) return launch_few<false>(epilogue, p, reinterpret_cast<const bf16_t *>(a.u), a.ld_u, a.k, s);
     return launch_few<true>(epilogue, p, nullptr, 0, a.k, s);
   }
-  // Tiles of 128 x 128, three workgroups a CU, as soon as every CU has one: their epilogues run under the others' products.  The residual
-  // update holds rows of the stream too and takes two a CU, and from two rounds of the chip on 256 x 256, which draws fewer operands
-  // through the L2.  us, 64 x 64 / 128 x 128 / 256 x 256: 2304 x 4608 x 1152 20.5 / 13.8 / 17.0, 48600 x 4608 x 1152 with GELU 340 / 205 / 246;
-  // residual 2304 x 1152 x 4608 20.9 / 22.7 / 40.4, 12960 87 / 59 / 62, 48600 366 / 262 / 247.  With two panels between barriers the small tile
-  // takes 20.3 and, 300 x 1152 x 4608, 10.4 in place of 12.3.
-  const int64_t t128 = ((a.N + 127) / 128) * ((a.n + 127) / 128), t256 = ((a.N + 255) / 256) * ((a.n + 255) / 256);
-  const int64_t cus = device_cus();
-  if (t128 < cus) return launch_tile<Mx4Cfg<64, 64, 2, 2, 2, 3, 2>>(epilogue, p, s);
+  if (f.cols == 64) return launch_tile<Mx4Cfg<64, 64, 2, 2, 2, 3, 2>>(epilogue, p, s);
+  if (f.cols == 256) return launch_tile<Mx4Cfg<256, 256, 2, 4, 3, 1>, true, false>(epilogue, p, s);
   if (epilogue != 2) return launch_tile<Mx4Cfg<128, 128, 2, 2, 2, 3>, false, true>(epilogue, p, s);
-  if (t256 < 2 * cus) return launch_tile<Mx4Cfg<128, 128, 2, 2, 3, 2>, true, false>(epilogue, p, s);
-  return launch_tile<Mx4Cfg<256, 256, 2, 4, 3, 1>, true, false>(epilogue, p, s);
+  return launch_tile<Mx4Cfg<128, 128, 2, 2, 3, 2>, true, false>(epilogue, p, s);
 }
 
 }  // namespace ddit
