@@ -483,13 +483,8 @@ int launch_form(int waves, const CrossParams &p, hipStream_t s) {
   return p.parts > 1 ? launch_as<KS, 8, ST, true>(p, s) : launch_as<KS, 8, ST, false>(p, s);
 }
 
-// Wavefronts of a workgroup, for `rows` rows a key head: one where sequences have few, on average; three a SIMD for heads whose registers allow it, from
-// two rounds of the chip on; else two.  us, 8 / 12, 16 heads of 72: 97200 rows x 300 states 245 / 233, 48600 x 1024 369 / 308, 2304 x 300 15.0 / 16.5; of 64
-// 97200 x 256 163 / 149; of 128 254 / 408.
-int waves_for(int B, int64_t rows, int H_kv, int dh) {
-  if (rows <= (int64_t)64 * B) return 1;
-  return dh <= 96 && rows * H_kv >= 512 * 256 ? 12 : 8;
-}
+// One wavefront a workgroup where sequences have few of the `rows` rows a key head, on average.
+bool lone_wavefronts(int B, int64_t rows) { return rows <= (int64_t)64 * B; }
 
 }  // namespace
 
@@ -500,7 +495,7 @@ namespace ddit {
 // fewer than 1024 states in all, where the second launch takes longer than what it saves (22 queries, 485 states: 10.9 us in 3 parts).
 int cross_attn_parts(int B, int64_t q_rows, int64_t kv_rows, int H, int H_kv) {
   const int64_t rows = q_rows * (H / H_kv);
-  const bool lone = waves_for(B, rows, H_kv, 0) == 1;
+  const bool lone = lone_wavefronts(B, rows);
   const int64_t units = (rows / (lone ? 32 : 256) + B) * H_kv;
   if (kv_rows < 1024) return 1;
   return (int)std::max<int64_t>(1, std::min<int64_t>({(int64_t)32, (lone ? 1024 : 256) / units, kv_rows / 128}));
@@ -510,8 +505,10 @@ CrossForm cross_attn_form(int B, int64_t q_rows, int64_t kv_rows, int H, int H_k
   const int64_t rows = q_rows * (H / H_kv);
   CrossForm f;
   f.parts = cross_attn_parts(B, q_rows, kv_rows, H, H_kv);
-  f.waves = waves_for(B, rows, H_kv, dh);
-  if (f.parts > 1) f.waves = std::min(8, f.waves);
+  // Three wavefronts a SIMD for heads whose registers allow it, from two rounds of the device on (256 rows a workgroup of eight); else two.
+  // us, 8 / 12, 16 heads of 72: 97200 rows x 300 states 245 / 233, 48600 x 1024 369 / 308, 2304 x 300 15.0 / 16.5; of 64 97200 x 256 163 / 149;
+  // of 128 254 / 408.
+  f.waves = lone_wavefronts(B, rows) ? 1 : f.parts == 1 && dh <= 96 && rows * H_kv >= (int64_t)512 * cus ? 12 : 8;
   f.run = 32 * f.waves;
   if (f.waves > 1 && f.parts == 1) {
     // row tiles a workgroup walks over: a round of the chip takes that many and about one more for its set-up; counted for sequences of one length

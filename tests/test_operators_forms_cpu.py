@@ -56,3 +56,10 @@ def test_attention_forms(m):
         for G in (1, 2, 4, 8, 16):
             parts = form(*totals, 16, G, 64)[1]
             assert parts == 1 or parts * totals[1] * 16 * 66 * 4 <= need
+
+
+def test_attention_forms_of_a_smaller_device(m):
+    """Two rounds of the chip are two of the device's: from 512 rows a compute unit on, counted over the key heads."""
+    for cus in (32, 64, 256):
+        form = lambda rows, dh: m.ddit_cross_attn_packed_form(1, rows, 300, 16, 16, dh, cus)[0]
+        assert form(32 * cus - 1, 72) == 8 and form(32 * cus, 72) == 12 and form(32 * cus, 104) == 8
