@@ -265,7 +265,8 @@ int ddit_self_attn_fwd(ddit_attn_kind kind, const ddit_shape *shape, void *q, vo
                        int64_t ld_o, float *lse_or_null, void *hip_stream);
 
 /* ---- operators of models that differ from the step's layers: norms behind a branch, linears in four bits, packed requests ----
- * A pointer to an array without elements (no token, no row, no encoder state) may be NULL. */
+ * A pointer to an array without elements (no token, no row, no encoder state) may be NULL, except c6: a call that asks for a gate or a
+ * modulation names its tables and c6 for no token too. */
 
 typedef enum { DDIT_NORM_LAYER = 0, DDIT_NORM_RMS = 1 } ddit_norm_kind;
 

@@ -9,8 +9,9 @@
 // g_pre * (1 + scale), shift: up to eight vectors to read for three to keep - is formed once per workgroup and kept in LDS,
 // so workgroups take runs of consecutive rows, cut where the sample changes.
 // One wavefront a row up to 2048 features; four share a row above, and below where rows are fewer than four a CU.
-// Measured: 48600 x 1152 139 us, 4.8 TB/s (a plain copy of that size 4.7), 12960 x 1152 40 us (29 with its operands in the memory-side
-// cache), 256 x 256 4.8 us.
+// Measured: 48600 x 1152 139 us, 4.8 TB/s (a plain copy of that size 4.6 to 4.7), 12960 x 1152 40 us (29 with its operands in the memory-side
+// cache), 256 x 256 4.8 us; four wavefronts a row: 12960 x 2304 88 us (4.1 TB/s), x 4096 142 (4.5), x 8192 332 (3.8; 96 KB of vectors leave one
+// workgroup a CU).
 #include "ddit_common.hpp"
 
 #include <algorithm>

@@ -18,9 +18,11 @@
 // dim have to be zeros: a weight of zero times an infinity would be NaN.  Up to 320 keys (256 of 128 features) are fetched once, and every
 // wavefront walks over its row tiles with no further barrier; longer sequences stream through two stages, one barrier a tile.
 //
-// Bound: the vector arithmetic of the softmax, some 150 instructions of 4 clocks and 32 exponentials a tile beside 22 matrix instructions of
-// 32 (2 x 48600 queries x 300 states x 16 heads of 72: 216 us, 620 TFLOP/s; each further tile of 64 keys 30 us), below 128 keys the
-// rows of q and o (143 us; a row of one head is 144 bytes, parts of two or three lines).
+// Bound, 2 x 48600 queries x 300 states x 16 heads of 72 (215 us, 620 TFLOP/s): the vector arithmetic of the softmax, at the clock that the
+// board's power leaves.  A wavefront issues 245 vector instructions a key tile, with its share of a row tile's begin and end, beside 22
+// matrix instructions of 32 clocks: vector issue takes 63 % of the SIMDs' time and the matrix cores 39 %, at 1400 W (the cap) and 1.93 of 2.4
+// GHz; wavefronts wait on loads and stores 29 % of theirs.  One state takes 150 us, 64 as long: up to two key tiles the rows of q and o
+// bound it (a row of one head is 144 bytes, parts of two or three lines).  192 states take 168, 256 184, 320 212.
 #include "ddit_common.hpp"
 
 #include <algorithm>
@@ -116,7 +118,8 @@ __global__ __launch_bounds__(64 * NW) void k_cross_attn(CrossParams p) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l32 = lane & 31, lh = lane >> 5;
   // Workgroups are dealt out to the 8 XCDs in turn.  The heads of a slot come one after the other on one XCD: a row of one head is 2 dh bytes
-  // of the token's, so heads share the cache lines of q and o, which its L2 puts together.
+  // of the token's, so heads share the cache lines of q and o, which its L2 puts together.  So do a slot's parts of the keys: where few slots
+  // have long encodings, an XCD reads all of a request's K and V by itself and others are idle.
   const int H_kv = p.H / p.group, i0 = blockIdx.x >> 3, i1 = i0 / H_kv, kv_head = i0 - i1 * H_kv;
   const int i2 = PARTS ? i1 / p.parts : i1, part = PARTS ? i1 - i2 * p.parts : 0;
   Slot slot;
@@ -223,7 +226,7 @@ __global__ __launch_bounds__(64 * NW) void k_cross_attn(CrossParams p) {
   // One tile: softmax of its scores and O^T += V^T P^T.  A wavefront issues in order, so the matrix instructions are threaded by hand through
   // the vector arithmetic, which takes longer than they do: one after every two exponentials, as soon as its 16 keys' weights are there.  V
   // fragments are read a chunk of 16 keys ahead.  (The next tile's scores in between as well, and room for them, changed nothing for 64 to 80
-  // features and spilled registers above: 2 x 48600 x 256 of 96 228 / 206 us, of 128 322 / 235.)
+  // features and spilled registers above: 2 x 48600 x 256 took a tenth longer with heads of 96, a third with heads of 128.)
   auto step = [&](int st, uint64_t bits, floatx16 (&s)[2]) {
     const unsigned valid[2] = {(unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)bits), (unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)(bits >> 32))};
     if ((valid[0] & valid[1]) != ~0u) {
@@ -324,13 +327,14 @@ __global__ __launch_bounds__(64 * NW) void k_cross_attn(CrossParams p) {
       return;
     }
     // Lanes without a row, or past the head dim, store past the end of the buffer, which drops it: the same stores for every tile, so that
-    // the wait for the next queries, which were asked for before them, need not be one for all stores.
+    // where the next queries were asked for before them (Q_AHEAD) the wait for those need not be one for all stores.  The other forms ask in
+    // begin, behind these stores, and wait for both.
     const float inv = l_run == 0.f ? 0.f : 1.f / l_run;
     const int q0 = r0 / p.group;   // first token of the tile
     const __amdgpu_buffer_rsrc_t r_o = buffer(p.o + (slot.q_first + q0) * p.ld_o + h0 * p.dh, 0x7fffffff);
     const unsigned o_at = in ? ((unsigned)(q - q0) * (unsigned)p.ld_o + (unsigned)((h - h0) * p.dh)) * 2u : NOWHERE;
     // Of 32 features lanes l and l + 32 hold groups of four in turn.  Two exchanges make it four lanes a row with eight features each, so that
-    // a store writes 64 bytes of 16 rows (with 32 bytes of 32 rows 97200 queries of one state took 150 us, without storing 88).
+    // a store writes 64 bytes of 16 rows in place of 32 bytes of 32.
     const unsigned at_lo = (unsigned)__shfl((int)o_at, lane & 15, 64), at_hi = (unsigned)__shfl((int)o_at, 16 + (lane & 15), 64);
     const int col_lane = 8 * (2 * ((lane >> 4) & 1) + lh);
 #pragma unroll
@@ -491,8 +495,10 @@ bool lone_wavefronts(int B, int64_t rows) { return rows <= (int64_t)64 * B; }
 namespace ddit {
 
 // From the totals alone, since the lengths are on the device, and for the whole chip whatever device is current, since the answer sizes workspaces:
-// parts of 128 keys and more, as many as make one round of the chip (a workgroup of eight wavefronts fills a CU, four of one do).  Not for
-// fewer than 1024 states in all, where the second launch takes longer than what it saves (22 queries, 485 states: 10.9 us in 3 parts).
+// parts of 128 keys and more, as many as make one round of the chip (a workgroup of eight wavefronts fills a CU, four of one do).  One part / as
+// taken, us in a captured graph: 22 queries of 16 heads of 72 x 1024 states 25.5 / 15.1 (8 parts), x 2048 46.5 / 20 (16), 1 x 4096 of 128 on 4
+// key heads 115 / 22 (32), 2000 x 4096 of 8 heads 99 / 53 (4).  From 1024 states in all on, a border that leaves time: 22 x 485 take 14.4 in one
+// part and 12.7 in three, 22 x 1000 25.3 and, in eight, 15.1; and 17 x 4096, whose rows want eight wavefronts, 39 in 32 parts and 26 in eight.
 int cross_attn_parts(int B, int64_t q_rows, int64_t kv_rows, int H, int H_kv) {
   const int64_t rows = q_rows * (H / H_kv);
   const bool lone = lone_wavefronts(B, rows);
@@ -506,8 +512,8 @@ CrossForm cross_attn_form(int B, int64_t q_rows, int64_t kv_rows, int H, int H_k
   CrossForm f;
   f.parts = cross_attn_parts(B, q_rows, kv_rows, H, H_kv);
   // Three wavefronts a SIMD for heads whose registers allow it, from two rounds of the device on (256 rows a workgroup of eight); else two.
-  // us, 8 / 12, 16 heads of 72: 97200 rows x 300 states 245 / 233, 48600 x 1024 369 / 308, 2304 x 300 15.0 / 16.5; of 64 97200 x 256 163 / 149;
-  // of 128 254 / 408.
+  // us, 8 / 12, 16 heads of 72: 2304 rows x 300 states 14.1 / 15.3, 6480 23.6 / 26.5, 8192 (the border) 24.5 / 28.5, 12960 39.9 / 40.6, 2 x 48600
+  // 236 / 215, 48600 x 1024 351 / 311; 2 x 48600 x 256 of 64 159 / 152, of 96 209 / 200, of 128 257 / 402.
   f.waves = lone_wavefronts(B, rows) ? 1 : f.parts == 1 && dh <= 96 && rows * H_kv >= (int64_t)512 * cus ? 12 : 8;
   f.run = 32 * f.waves;
   if (f.waves > 1 && f.parts == 1) {

@@ -185,11 +185,12 @@ __device__ __forceinline__ bool tile_of(const Mx4Params &p, int round, int &tile
 // direct global -> LDS loads NS - 1 panels ahead; the stream of panels runs on into the workgroup's next tile, whose first panels
 // thus arrive ahead of the stores of this one.  A row's four 16-byte pieces are stored in the order piece ^ (row / 4 % 4), which spreads
 // the 16 rows that an LDS read serves at a time over all banks; the loads fetch them from there.
-// Bound: 48600 x 4608 x 1152 (205-228 us, 2.3-2.5 PFLOP/s; bf16 out 175-190) spends 85-97 us of it in matrix instructions alone, at the 1.8-2.0
-// GHz that the power limit leaves, 20 in LDS reads, 25 in loads, 30 to 55 in the epilogue's arithmetic and stores (each measured by leaving
-// the others out).  Rows leave through LDS in pieces of 128 bytes: whole lines.  Straight from the registers, after lane exchanges,
-// in pieces of 64 bytes, they took 213 us with GELU, 219 without and 290 to 350 in place of 250 in the residual update.  Reading the next
-// step's fragments under the products of this one: 0 to 6 % longer.
+// Bound, 48600 x 4608 x 1152 with GELU (213 us, 2.4 PFLOP/s; bf16 out 183): the board's power, 1400 W (the cap) at 1.96 of 2.4 GHz (bf16 out
+// 1.76), with no unit busy all of the time: vector issue 53 % of the SIMDs' (GELU and the epilogue), the matrix cores 29 %, the LDS 28 % of
+// the CUs' time.  The residual update of 48600 x 1152 x 4608 (243 us, 2.1 PFLOP/s) comes to 1385 W at 2.29 GHz and waits: matrix cores 24 %,
+// wavefronts on loads and stores 30 % of their time.  Rows leave through LDS in pieces of 128 bytes: whole lines.  Straight from the registers,
+// after lane exchanges, in pieces of 64 bytes, they took 4 % longer with GELU, a quarter longer without and 16 to 40 % longer in the
+// residual update.  Reading the next step's fragments under the products of this one: 0 to 6 % longer.
 template <class C, int EPI>
 __global__ __launch_bounds__(64 * C::NW, C::NW * C::PER_CU / 4) void k_mx4_gemm(Mx4Params p) {
   constexpr int BM = C::BM, BN = C::BN, NW = C::NW, TM = C::TM, TN = C::TN, NS = C::NS;
@@ -542,8 +543,8 @@ int launch_few(int epi, const Mx4Params &p, const bf16_t *u, int64_t ld_u, int k
 }
 
 // Every workgroup quantises all tokens, so with more than 16 of them it pays where workgroups are few.  us in a captured graph, one launch / two:
-// 16 tokens of 1152 x 1152 3.8 / 7.5, 6912 x 1152 5.2 / 7.8, 1152 x 4608 7.3 / 13.8; 32 tokens 5.5 / 7.5, 9.6 / 7.8, 12.4 / 13.8; 64 tokens
-// 8.8 / 7.5, 17.3 / 7.8, 22.9 / 13.8.
+// 16 tokens of 1152 x 1152 3.7 / 7.1, 6912 x 1152 5.0 / 7.2, 1152 x 4608 7.3 / 13.1; 32 tokens 5.4 / 7.2, 9.4 / 7.3, 12.2 / 13.6 and of
+// 2304 x 1152, past the border, 5.5 / 7.2; 64 tokens 8.8 / 7.5, 16.7 / 7.6, 22.7 / 13.8.
 bool few_tokens(int64_t N, int n) { return N <= 16 || (N <= 32 && n <= 2048); }
 
 template <class C, int EPI>
@@ -595,9 +596,11 @@ Mx4Form mx4_form(int epilogue, int64_t N, int n, int cus) {
   if (few_tokens(N, n)) return {N <= 16 ? 16 : 32, 16};
   // Tiles of 128 x 128, three workgroups a CU, as soon as every CU has one: their epilogues run under the others' products.  The residual
   // update holds rows of the stream too and takes two a CU, and from two rounds of the chip on 256 x 256, which draws fewer operands
-  // through the L2.  us, 64 x 64 / 128 x 128 / 256 x 256: 2304 x 4608 x 1152 20.5 / 13.8 / 17.0, 48600 x 4608 x 1152 with GELU 340 / 205 / 246;
-  // residual 2304 x 1152 x 4608 20.9 / 22.7 / 40.4, 12960 87 / 59 / 62, 48600 366 / 262 / 247.  With two panels between barriers the small tile
-  // takes 20.3 and, 300 x 1152 x 4608, 10.4 in place of 12.3.
+  // through the L2.  us, 64 x 64 / 128 x 128 / 256 x 256, u in codes: with GELU 2304 x 4608 x 1152 20.8 / 12.3 / 15.4, 12960 101 / 59.8 / 57.9, 48600
+  // 370 / 213 / 202; bf16 out 300 x 2304 x 1152 5.2 / 6.5 / 11.8, 12960 x 1152 x 1152 27.5 / 14.2 / 15.3, 48600 x 1152 x 4608 - / 145 / 151,
+  // 48600 x 4608 x 1152 350 / 183 / 168; residual 2304 x 1152 x 4608 20.3 / 20.8 / 40.9, 6480 44 / 30 / 44, 12960 87 / 59 / 60, 48600 387 / 264 / 243.
+  // So many tokens of many features and a short k would gain 5 to 8 % from 256 x 256 without a stream too, which is not compiled.  With two panels
+  // between barriers in place of one the small tile takes, 300 x 1152 x 4608, 10.1 in place of 10.9 and, residual, 6480 44 in place of 49.
   const int64_t t128 = ((N + 127) / 128) * ((n + 127) / 128), t256 = ((N + 255) / 256) * ((n + 255) / 256);
   if (t128 < cus) return {64, 64};
   if (epilogue != 2 || t256 < 2 * cus) return {128, 128};
